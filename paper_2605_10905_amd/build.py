@@ -1,4 +1,4 @@
-"""Builds the HIP library in-tree (hipcc, gfx950 only).  `python -m paper_2605_10905_amd.build`."""
+"""Builds the HIP libraries in-tree (hipcc, gfx950 only).  `python -m paper_2605_10905_amd.build`."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libattn_mi355x.so")
 SOURCES = ["attn_api.hip", "attn_fwd_sp.hip", "attn_fwd_fp8.hip", "attn_bwd_bf16.hip", "gemm_api.hip", "gemm_bf16.hip", "gemm_wavek.hip"]
+# what stands around attention in a layer (include/kv.h) is a library of its own: who only attends does not load it
+LIB_KV = os.path.join(HERE, "libkv_mi355x.so")
+SOURCES_KV = ["kv_api.hip", "rope.hip", "kv_decode.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 VALU forms are switched off on purpose (they have misbehaved on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -21,15 +24,15 @@ SOURCE_FLAGS = {"attn_bwd_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def build(verbose: bool = True, extra_flags=()) -> str:
-    objs = []
+    objs = {}
     procs = []
-    for src in SOURCES:
+    for src in SOURCES + SOURCES_KV:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
         cmd = [HIPCC, *FLAGS, *SOURCE_FLAGS.get(src, []), *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-        objs.append(obj)
+        objs[src] = obj
     for cmd, pr in procs:
         out, _ = pr.communicate()
         out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
@@ -37,10 +40,11 @@ def build(verbose: bool = True, extra_flags=()) -> str:
             raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + out)
         if verbose and out.strip():
             print(out)
-    cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    for lib, sources in ((LIB, SOURCES), (LIB_KV, SOURCES_KV)):
+        cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *[objs[src] for src in sources], "-o", lib]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
     return LIB
 
 

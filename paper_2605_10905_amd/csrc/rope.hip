@@ -1,0 +1,359 @@
+// Split, per-head RMS norm and rotation of a packed q|k|v projection (rope_qkv), its gradients (rope_qkv_bwd), and the same
+// into a paged cache (kv_append).
+//
+// One pass over the rows, bound by memory: a row of d features is read once, everything between is 32-bit arithmetic in
+// registers, and it is rounded once when it is written.  d / 16 lanes hold a row, each two 16-byte chunks a and b, chosen so
+// that every pair of rotated features lies in one lane: chunk c of the first rot / 16 and chunk c + rot / 16, whose features
+// are each other's partners when the pairs are (f, f + rot / 2); adjacent pairs lie inside a chunk anyhow.  What is not
+// rotated is dealt to the remaining lanes the same way.  The mean of squares is a sum over d / 16 neighbouring lanes (quad
+// permutations and a half-row mirror, no LDS).
+#include "attn_device.h"
+#include "kv_kernels.h"
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kMostWorkgroups = 1 << 20;  // (a launch holds 2^32 threads)
+
+// sum over the LPR (4 or 8) neighbouring lanes of a row, the same value in all of them
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xF, 0xF, true));   // quad_perm 1,0,3,2
+  x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xF, 0xF, true));   // quad_perm 2,3,0,1
+  if constexpr (LPR == 8) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xF, 0xF, true));  // row_half_mirror
+  return x;
+}
+
+__device__ __forceinline__ void unpack(const u32x4 x, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(x[i] << 16);
+    f[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
+  return u32x4{attn_pack_bf16(f[0], f[1]), attn_pack_bf16(f[2], f[3]), attn_pack_bf16(f[4], f[5]), attn_pack_bf16(f[6], f[7])};
+}
+
+// which two chunks lane j of a row holds, and whether they are rotated
+struct Chunks {
+  int a, b;
+  bool rotated;
+};
+template <int LPR>
+__device__ __forceinline__ Chunks chunks_of(int j, int rot) {
+  const int r = rot >> 4;
+  Chunks c;
+  c.rotated = j < r;
+  c.a = j < r ? j : r + j;
+  c.b = j < r ? j + r : LPR + j;
+  return c;
+}
+
+// cosine and sine of the lane's eight pairs at position `pos` (inside the table); 1 and 0 where nothing is rotated
+__device__ __forceinline__ void load_angles(const RopeParams& p, const Chunks& c, int pos, float (&cs)[8], float (&sn)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = 1.f;
+    sn[i] = 0.f;
+  }
+  if (!c.rotated) return;
+  typedef __attribute__((ext_vector_type(4))) float f32x4;
+  const f32x4* const row = (const f32x4*)(p.table + (size_t)pos * p.rot);
+  const int at0 = p.interleaved ? 2 * c.a : 4 * c.a, at1 = p.interleaved ? 2 * c.b : 4 * c.a + 2;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x4 t = row[(i < 2 ? at0 : at1) + (i & 1)];
+    cs[2 * i] = t[0];
+    sn[2 * i] = t[1];
+    cs[2 * i + 1] = t[2];
+    sn[2 * i + 1] = t[3];
+  }
+}
+
+// the rotation (SIGN 1) or its transpose (-1)
+template <int SIGN>
+__device__ __forceinline__ void rotate(bool interleaved, float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) {
+  if (!interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float s = SIGN * sn[i], x = a[i], y = b[i];
+      a[i] = x * cs[i] - y * s;
+      b[i] = y * cs[i] + x * s;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float s = SIGN * sn[i], x = a[2 * i], y = a[2 * i + 1];
+      a[2 * i] = x * cs[i] - y * s;
+      a[2 * i + 1] = y * cs[i] + x * s;
+      const float s2 = SIGN * sn[4 + i], x2 = b[2 * i], y2 = b[2 * i + 1];
+      b[2 * i] = x2 * cs[4 + i] - y2 * s2;
+      b[2 * i + 1] = y2 * cs[4 + i] + x2 * s2;
+    }
+  }
+}
+
+template <int LPR>
+__device__ __forceinline__ float inverse_rms(const float (&a)[8], const float (&b)[8], float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += a[i] * a[i] + b[i] * b[i];
+  // 1 / sqrt, not the approximate reciprocal root: a row's error would be common to all of its features
+  return 1.f / sqrtf(row_sum<LPR>(s) * (1.f / (16 * LPR)) + eps);
+}
+
+// eight codes of x / descale, round to nearest even, saturated; NaN stays NaN
+__device__ __forceinline__ u32x2 to_e4m3(const float (&x)[8], float descale) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y[i] = x[i] / descale;
+    y[i] = y[i] > 448.f ? 448.f : y[i] < -448.f ? -448.f : y[i];
+  }
+  int w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], w[i], false);
+    w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], w[i], true);
+  }
+  return u32x2{(uint32_t)w[0], (uint32_t)w[1]};
+}
+
+enum { kLayout = 0, kCacheBf16 = 1, kCacheFp8 = 2 };
+
+// 64 / (d / 16) consecutive heads of one token, by one wave
+template <int D, int MODE>
+__device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int task) {
+  constexpr int LPR = D / 16, RPW = 64 / LPR;
+  const int lane = threadIdx.x & 63;
+  const int t = task / groups, h = (task % groups) * RPW + lane / LPR, j = lane % LPR;
+  const int H = p.Hq + 2 * p.Hkv;
+  if (h >= H) return;
+  const Chunks c = chunks_of<LPR>(j, p.rot);
+
+  int pos = p.pos ? p.pos[t] : t % (p.N > 0 ? p.N : 1);
+  int entry = -1, seq = 0;
+  bool good = p.rot == 0 || (unsigned)pos < (unsigned)p.npos;
+  if constexpr (MODE != kLayout) {
+    if (pos < 0) return;  // padding
+    good = p.rot == 0 || pos < p.npos;
+    seq = p.seq ? p.seq[t] : t;
+    good = good && (unsigned)seq < (unsigned)p.S;
+    if (good && (pos >> p.page_log2) < p.W) entry = p.pages[(size_t)seq * p.W + (pos >> p.page_log2)];
+    if ((unsigned)entry >= (unsigned)p.num_pages) entry = -1;
+  }
+
+  const char* const src = (const char*)p.qkv + ((size_t)t * p.ld + (size_t)h * D) * 2;
+  const u32x4 xa = *(const u32x4*)(src + c.a * 16), xb = *(const u32x4*)(src + c.b * 16);
+  const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
+  float a[8], b[8];
+  unpack(xa, a);
+  unpack(xb, b);
+  if (!is_v) {
+    if (p.wq) {
+      const char* const wsrc = (const char*)(is_q ? p.wq : p.wk);
+      float wa[8], wb[8];
+      unpack(*(const u32x4*)(wsrc + c.a * 16), wa);
+      unpack(*(const u32x4*)(wsrc + c.b * 16), wb);
+      const float r = inverse_rms<LPR>(a, b, p.eps);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a[i] = a[i] * r * wa[i];
+        b[i] = b[i] * r * wb[i];
+      }
+    }
+    float cs[8], sn[8];
+    load_angles(p, c, good ? pos : 0, cs, sn);
+    rotate<1>(p.interleaved, a, b, cs, sn);
+    if (!good) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
+    }
+  }
+
+  const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
+  char* dst;
+  if constexpr (MODE == kLayout) {
+    const int n = t % p.N, bb = t / p.N, Hk = is_q ? p.Hq : p.Hkv;
+    dst = (char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
+  } else if (is_q) {
+    dst = (char*)p.q + ((size_t)t * p.Hq + hk) * (D * 2);
+  } else {
+    if (!good || entry < 0) return;
+    const size_t row = (((size_t)entry * p.Hkv + hk) << p.page_log2) + (pos & ((1 << p.page_log2) - 1));
+    dst = (char*)(is_v ? p.v : p.k) + row * (D * (MODE == kCacheFp8 ? 1 : 2));
+    if constexpr (MODE == kCacheFp8) {
+      const float descale = is_v ? p.v_descale : p.k_descale;
+      *(u32x2*)(dst + c.a * 8) = to_e4m3(a, descale);
+      *(u32x2*)(dst + c.b * 8) = to_e4m3(b, descale);
+      return;
+    }
+  }
+  *(u32x4*)(dst + c.a * 16) = is_v ? xa : pack(a);
+  *(u32x4*)(dst + c.b * 16) = is_v ? xb : pack(b);
+}
+
+template <int D, int MODE>
+__global__ void __launch_bounds__(kWaves * 64) rope_qkv_kernel(const RopeParams p, int groups, int tasks) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) rope_task<D, MODE>(p, groups, task);
+}
+
+// The gradients.  A workgroup walks tasks (a token's 64 / (d / 16) heads) a grid apart and keeps what its lanes add to the
+// weights' gradients in registers; the sums over lanes, waves and workgroups follow in a fixed order.
+template <int D, bool NORM>
+__global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopeParams p, int groups, int tasks) {
+  constexpr int LPR = D / 16, RPW = 64 / LPR;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int j = lane % LPR, H = p.Hq + 2 * p.Hkv;
+  const Chunks c = chunks_of<LPR>(j, p.rot);
+  float acc[2][2][8];  // [q, k][chunk a, b]
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[0][0][i] = acc[0][1][i] = acc[1][0][i] = acc[1][1][i] = 0.f;
+
+  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) {
+    const int t = task / groups, h = (task % groups) * RPW + lane / LPR;
+    if (h >= H) continue;
+    const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
+    const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq, Hk = is_q ? p.Hq : p.Hkv;
+    const int n = t % p.N, bb = t / p.N;
+    const char* const src = (const char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
+    char* const dst = (char*)p.dqkv + ((size_t)t * p.dld + (size_t)h * D) * 2;
+    const u32x4 ga4 = *(const u32x4*)(src + c.a * 16), gb4 = *(const u32x4*)(src + c.b * 16);
+    if (is_v) {
+      *(u32x4*)(dst + c.a * 16) = ga4;
+      *(u32x4*)(dst + c.b * 16) = gb4;
+      continue;
+    }
+    const int pos = p.pos ? p.pos[t] : n;
+    const bool good = p.rot == 0 || (unsigned)pos < (unsigned)p.npos;
+    float a[8], b[8], cs[8], sn[8];
+    unpack(ga4, a);
+    unpack(gb4, b);
+    load_angles(p, c, good ? pos : 0, cs, sn);
+    rotate<-1>(p.interleaved, a, b, cs, sn);
+    if (!good) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
+    }
+    if constexpr (NORM) {
+      const char* const xsrc = (const char*)p.qkv + ((size_t)t * p.ld + (size_t)h * D) * 2;
+      const char* const wsrc = (const char*)(is_q ? p.wq : p.wk);
+      float xa[8], xb[8], wa[8], wb[8];
+      unpack(*(const u32x4*)(xsrc + c.a * 16), xa);
+      unpack(*(const u32x4*)(xsrc + c.b * 16), xb);
+      unpack(*(const u32x4*)(wsrc + c.a * 16), wa);
+      unpack(*(const u32x4*)(wsrc + c.b * 16), wb);
+      const float r = inverse_rms<LPR>(xa, xb, p.eps);
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        xa[i] *= r;
+        xb[i] *= r;
+        const float da = a[i] * xa[i], db = b[i] * xb[i];
+        acc[0][0][i] += is_q ? da : 0.f;
+        acc[0][1][i] += is_q ? db : 0.f;
+        acc[1][0][i] += is_q ? 0.f : da;
+        acc[1][1][i] += is_q ? 0.f : db;
+        a[i] *= wa[i];
+        b[i] *= wb[i];
+        dot += a[i] * xa[i] + b[i] * xb[i];
+      }
+      dot = row_sum<LPR>(dot) * (1.f / D);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a[i] = r * (a[i] - xa[i] * dot);
+        b[i] = r * (b[i] - xb[i] * dot);
+      }
+    }
+    *(u32x4*)(dst + c.a * 16) = pack(a);
+    *(u32x4*)(dst + c.b * 16) = pack(b);
+  }
+
+  if constexpr (NORM) {
+    // over the rows a wave holds at once (lanes that agree mod LPR), then over the waves
+    __shared__ float part[kWaves][2][D];
+#pragma unroll
+    for (int qk = 0; qk < 2; ++qk)
+#pragma unroll
+      for (int ab = 0; ab < 2; ++ab)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float x = acc[qk][ab][i];
+#pragma unroll
+          for (int m = LPR; m < 64; m *= 2) x += __shfl_xor(x, m);
+          if (lane < LPR) part[w][qk][(ab ? c.b : c.a) * 8 + i] = x;
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * D; i += kWaves * 64) {
+      float x = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) x += part[k][i / D][i % D];
+      p.partial[(size_t)blockIdx.x * (2 * D) + i] = x;
+    }
+  }
+}
+
+// the sums over workgroups: one workgroup for 16 of the 2 d columns, 16 threads each
+template <int D>
+__global__ void __launch_bounds__(256) rope_weight_sum_kernel(const float* partial, int workgroups, float* dwq, float* dwk) {
+  __shared__ float part[16][16];
+  const int col = blockIdx.x * 16 + (threadIdx.x & 15), at = threadIdx.x >> 4;
+  float x = 0.f;
+  for (int i = at; i < workgroups; i += 16) x += partial[(size_t)i * (2 * D) + col];
+  part[at][threadIdx.x & 15] = x;
+  __syncthreads();
+  if (at == 0) {
+    x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x += part[i][threadIdx.x];
+    (col < D ? dwq : dwk)[col % D] = x;
+  }
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
+
+int tasks_of(const RopeParams& p, int d, int* groups) {
+  const int rows = 1024 / d;  // heads a wave takes at once
+  *groups = (p.Hq + 2 * p.Hkv + rows - 1) / rows;
+  return p.T * *groups;  // (at most T * heads, which fits)
+}
+
+template <int MODE>
+int launch_rows(const RopeParams& p, int d, hipStream_t stream) {
+  int groups;
+  const int tasks = tasks_of(p, d, &groups), grid = min((tasks - 1) / kWaves + 1, kMostWorkgroups);
+  if (d == 128) rope_qkv_kernel<128, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+  else rope_qkv_kernel<64, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+  return launched();
+}
+
+}  // namespace
+
+int rope_qkv_launch(const RopeParams& p, int d, hipStream_t stream) { return launch_rows<kLayout>(p, d, stream); }
+
+int kv_append_launch(const RopeParams& p, int d, bool fp8, hipStream_t stream) {
+  return fp8 ? launch_rows<kCacheFp8>(p, d, stream) : launch_rows<kCacheBf16>(p, d, stream);
+}
+
+int rope_qkv_bwd_workgroups(long long T, long long heads, int d) {
+  const long long rows = d >= 1024 ? 1 : 1024 / d, tasks = T * ((heads + rows - 1) / rows), wgs = (tasks + kWaves - 1) / kWaves;
+  return (int)(wgs < 1024 ? wgs : 1024);
+}
+
+int rope_qkv_bwd_launch(const RopeParams& p, int d, hipStream_t stream) {
+  int groups;
+  const int tasks = tasks_of(p, d, &groups), grid = rope_qkv_bwd_workgroups(p.T, p.Hq + 2 * p.Hkv, d);
+  if (p.wq) {
+    if (d == 128) rope_qkv_bwd_kernel<128, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+    else rope_qkv_bwd_kernel<64, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+    if (launched() != 0) return 1;
+    if (d == 128) rope_weight_sum_kernel<128><<<2 * 128 / 16, 256, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
+    else rope_weight_sum_kernel<64><<<2 * 64 / 16, 256, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
+  } else {
+    if (d == 128) rope_qkv_bwd_kernel<128, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+    else rope_qkv_bwd_kernel<64, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+  }
+  return launched();
+}
