@@ -28,7 +28,7 @@ int check_rows(const void* qkv, bool need_qkv, long long ld, const void* wq, con
 int check_pages(int W, int page_size, int num_pages) {
   if (W <= 0 || page_size <= 0 || num_pages <= 0) return ATTN_ERR_SHAPE;
   if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)) != 0) return ATTN_ERR_UNSUPPORTED;
-  if ((long long)W * page_size > 0x7fffffffll) return ATTN_ERR_UNSUPPORTED;
+  if ((long long)W * page_size > (1ll << 30)) return ATTN_ERR_UNSUPPORTED;
   return ATTN_OK;
 }
 

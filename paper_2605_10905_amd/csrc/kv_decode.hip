@@ -1,73 +1,526 @@
 // Attention of one new token per sequence over the paged cache (kv_decode).
+//
+// The call reads every visible key and value once and does 4 G operations on each of their features (G query heads share a
+// key head), so it is bound by memory as long as the products run on the matrix cores and enough bytes are in flight.
+//
+// Split: the work is the list of all 32-key tiles, sequence by sequence, key head by key head; each of kWorkers waves takes an
+// equal, consecutive piece of it, whatever the lengths are.  What the pieces are follows from `lens` on the device, by a scan over them
+// that every wave does for itself.  A wave that covers all tiles of a (sequence, key head) writes its rows of o; a wave that covers
+// some of them leaves its sums (32 bits) in the workspace, at most two per wave (where its piece begins and where it ends), and the
+// second kernel joins them.
+//
+// A wave streams its tiles through a ring of its own in LDS (32 KB: 128 KB of a CU's four waves, of which at least half is in flight),
+// by direct-to-LDS loads, so that no barrier is needed anywhere.  Page entries come through the scalar cache, whose counter is not the
+// tiles'.  A 16-row half of a tile lies in one page (pages hold 16 rows or more).
+//
+// Products are taken transposed, as in attn_fwd: S^T = K Q^T and O^T += V^T P^T on the 16x16x32 MFMA, the queries of the
+// group as its 16 columns (NQ blocks of them, fed by the same keys).  A lane then holds keys 4 g + r of both halves of a tile for one query, which
+// are the eight k of its second operand in place: key 4 g + r of half e is k = 8 g + 4 e + r, and V is read (transposing LDS loads)
+// in the same order.
+#include <type_traits>
+
 #include "attn_device.h"
 #include "kv_kernels.h"
 
 namespace {
 
-constexpr int kWaves = 4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
 
-__device__ __forceinline__ float element(const char* row, int i, bool fp8) {
-  if (!fp8) return __uint_as_float((uint32_t)((const uint16_t*)row)[i] << 16);
-  return __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)row)[i], 0);
+constexpr int kWaves = 4, kWorkers = 1024, kWorkersLog2 = 10;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// a value that all lanes agree on, in a scalar register
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ unsigned long long uniform(unsigned long long x) {
+  return (unsigned long long)(uint32_t)uniform((int)(uint32_t)x) | ((unsigned long long)(uint32_t)uniform((int)(x >> 32)) << 32);
+}
+// scalar load of what no kernel writes while this one runs
+__device__ __forceinline__ int scalar_load(const int* p, size_t i) { return ((const __attribute__((address_space(4))) int*)p)[i]; }
+
+__device__ __forceinline__ int visible_keys(const DecodeParams& p, int len) { return min(max(len, 0), p.W << p.page_log2); }
+__device__ __forceinline__ int tiles_of(int keys) { return (keys + 31) >> 5; }
+
+// All tiles of one key head: the sum over the sequences.
+__device__ __forceinline__ unsigned long long count_tiles(const DecodeParams& p) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long mine = 0;
+  for (int b = lane; b < p.B; b += 64) mine += tiles_of(visible_keys(p, p.lens[b]));
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) mine += __shfl_xor(mine, m);
+  return uniform(mine);
 }
 
-// One workgroup per query row; its waves take the keys in turn, lane i the features i and i + 64.
-template <int D, bool FP8>
-__global__ void __launch_bounds__(kWaves * 64) kv_decode_kernel(const DecodeParams p) {
-  constexpr int E = D / 64;
-  __shared__ float so[kWaves][D], sm[kWaves], sl[kWaves];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int b = blockIdx.x / p.Hq, hq = blockIdx.x % p.Hq, hk = hq / (p.Hq / p.Hkv);
-  const int len = min(max(p.lens[b], 0), p.W << p.page_log2);
-  const uint16_t* const qrow = (const uint16_t*)p.q + (size_t)blockIdx.x * D;
-  float q[E], o[E], m = -__builtin_inff(), l = 0.f;
-  for (int e = 0; e < E; ++e) {
-    q[e] = __uint_as_float((uint32_t)qrow[lane + 64 * e] << 16);
-    o[e] = 0.f;
+// Tiles of one key head in front of every sequence of the 64 from `first` on (lane by lane), given those in front of `first`; their
+// sum fits 32 bits (2^25 tiles a sequence).
+__device__ __forceinline__ uint32_t scan64(uint32_t x) {
+  const int lane = threadIdx.x & 63;
+  uint32_t sum = x;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const uint32_t y = __shfl_up(sum, m);
+    if (lane >= m) sum += y;
   }
-  for (int j = w; j < len; j += kWaves) {
-    const int entry = p.pages[(size_t)b * p.W + (j >> p.page_log2)];
-    if ((unsigned)entry >= (unsigned)p.num_pages) continue;
-    const size_t row = ((((size_t)entry * p.Hkv + hk) << p.page_log2) + (j & ((1 << p.page_log2) - 1))) * (D * (FP8 ? 1 : 2));
-    float s = 0.f;
-    for (int e = 0; e < E; ++e) s += q[e] * element((const char*)p.k + row, lane + 64 * e, FP8);
-    for (int x = 1; x < 64; x *= 2) s += __shfl_xor(s, x);
-    const float m_new = fmaxf(m, s), ref = m_new == -__builtin_inff() ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2), pr = __builtin_amdgcn_exp2f((s - ref) * p.scale_log2);
-    for (int e = 0; e < E; ++e) o[e] = o[e] * alpha + pr * element((const char*)p.v + row, lane + 64 * e, FP8);
-    l = l * alpha + pr;
+  return sum;
+}
+
+struct Place {
+  int b, len;                 // the sequence and its visible keys
+  unsigned long long before;  // tiles of one key head in front of it
+};
+// The sequence that tile `at` of the list (units x tiles of each sequence) belongs to.
+__device__ __forceinline__ Place place_of(const DecodeParams& p, unsigned long long at, int units) {
+  const int lane = threadIdx.x & 63;
+  Place r = {0, 0, 0};
+  unsigned long long base = 0;
+  for (int first = 0; first < p.B; first += 64) {
+    const int len = first + lane < p.B ? visible_keys(p, p.lens[first + lane]) : 0;
+    const uint32_t own = tiles_of(len), incl = scan64(own);
+    const unsigned long long before = base + (incl - own);
+    const int n = __popcll(__ballot(first + lane < p.B && before * (unsigned)units <= at));
+    if (n == 0) break;
+    r.b = first + n - 1;
+    r.len = __builtin_amdgcn_readlane(len, n - 1);
+    r.before = base + (uint32_t)__builtin_amdgcn_readlane((int)(incl - own), n - 1);
+    if (n < 64) break;
+    base += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+  }
+  return r;
+}
+
+__device__ __forceinline__ float max_rows(float x) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return attn_max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_rows(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return attn_sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ bf16x8 e4m3_to_bf16(uint32_t lo, uint32_t hi) {  // (exact)
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  return __builtin_bit_cast(bf16x8, o);
+}
+
+// query heads that one unit of the list takes, and units of a sequence
+__host__ __device__ constexpr int blocks_for(int G) { return G <= 16 ? 1 : G <= 32 ? 2 : 4; }
+__host__ __device__ __forceinline__ int rows_kept(int G) { return G < 16 * blocks_for(G) ? G : 16 * blocks_for(G); }
+// floats of one wave's sums: rows of O, then (reference maximum, sum) of each row
+__host__ __device__ __forceinline__ int partial_floats(int rows, int d) { return rows * d + (2 * rows + 3) / 4 * 4; }
+
+template <int D, bool FP8, int NQ>
+__global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeParams p) {
+  constexpr int ROWB = D * (FP8 ? 1 : 2), NCH = ROWB / 16, TILEB = 32 * ROWB;
+  constexpr int LPT = TILEB / 1024, PIECE_ROWS = 1024 / ROWB;  // direct loads of a tile of keys or values, rows of one
+  constexpr int RING = 32768 / (2 * TILEB), NDB = D / 16, NKS = D / 32;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * 32768];
+  LDS_AS char* const smem = (LDS_AS char*)smem_raw;
+
+  const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, j16 = lane & 15, g = lane >> 4;
+  const int worker = blockIdx.x * kWaves + w;
+  const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG;
+  const int page_mask = (1 << p.page_log2) - 1;
+
+  const unsigned long long all = count_tiles(p) * (unsigned)units;
+  const unsigned long long begin = (all * worker) >> kWorkersLog2, end = (all * (worker + 1)) >> kWorkersLog2;
+  if (begin == end) return;
+  int n = (int)(end - begin);  // (at most 2^59 / 2^10 tiles are ever asked for; a cache that fits the memory has far below 2^31)
+  const Place at = place_of(p, begin, units);
+
+  // A position in the list: tile t of `unit` of sequence b, and what its two page entries are
+  struct Position {
+    int b, unit, t, nt, len, e0, e1;
+  };
+  auto entries = [&](Position& x) __attribute__((always_inline)) {
+    const int j = x.t << 5;
+    const size_t row = (size_t)x.b * p.W;
+    x.e0 = scalar_load(p.pages, row + (j >> p.page_log2));
+    x.e1 = j + 16 < x.len ? scalar_load(p.pages, row + ((j + 16) >> p.page_log2)) : -1;
+  };
+  auto advance = [&](Position& x) __attribute__((always_inline)) {
+    if (++x.t < x.nt) return;
+    x.t = 0;
+    if (++x.unit < units) return;
+    x.unit = 0;
+    do {  // (there is another tile: no more are asked for than the list has)
+      if (x.b + 1 >= p.B) break;
+      ++x.b;
+      x.len = visible_keys(p, scalar_load(p.lens, x.b));
+    } while (x.len == 0);
+    x.nt = tiles_of(x.len);
+  };
+  Position ld;
+  {
+    const unsigned long long rest = begin - at.before * (unsigned)units;
+    ld.b = at.b;
+    ld.len = at.len;
+    ld.nt = tiles_of(at.len);
+    ld.unit = uniform((int)(rest / (unsigned)ld.nt));
+    ld.t = uniform((int)(rest - (unsigned long long)ld.unit * (unsigned)ld.nt));
+  }
+  Position cp = ld;
+  entries(ld);
+
+  // ---- direct loads: piece c of a half tile is rows c * PIECE_ROWS + lane / NCH; chunks are swizzled on the global side ----
+  uint32_t koff[LPT / 2], voff[LPT / 2];
+#pragma unroll
+  for (int c = 0; c < LPT / 2; ++c) {
+    const int r = c * PIECE_ROWS + lane / NCH, ch = lane % NCH;
+    koff[c] = r * ROWB + ((ch ^ attn_swz_k<ROWB>(r)) << 4);
+    voff[c] = r * ROWB + ((ch ^ (FP8 ? attn_swz_k<ROWB>(r) : attn_swz_v<ROWB>(r))) << 4);
+  }
+  const uint32_t ring = (uint32_t)(uintptr_t)smem + w * 32768;
+  // requests tile `ld` into `slot`; the result tells which of its halves have a page.  What has none is read from where the other half
+  // lies (or the cache's first rows) and hidden later.
+  auto issue = [&](int slot) __attribute__((always_inline)) {
+    const int j = ld.t << 5, hk = ld.unit / QG;
+    const bool ok0 = (unsigned)ld.e0 < (unsigned)p.num_pages, ok1 = (unsigned)ld.e1 < (unsigned)p.num_pages;
+    const size_t a0 = ok0 ? ((((size_t)ld.e0 * p.Hkv + hk) << p.page_log2) + (j & page_mask)) * ROWB : 0;
+    const size_t a1 = ok1 ? ((((size_t)ld.e1 * p.Hkv + hk) << p.page_log2) + ((j + 16) & page_mask)) * ROWB : a0;
+    const char* const k = (const char*)p.k;
+    const char* const v = (const char*)p.v;
+    const uint32_t to = ring + slot * (2 * TILEB);
+#pragma unroll
+    for (int c = 0; c < LPT; ++c) attn_lds_dma16(k + (c < LPT / 2 ? a0 : a1), koff[c % (LPT / 2)], to + c * 1024);
+#pragma unroll
+    for (int c = 0; c < LPT; ++c) attn_lds_dma16(v + (c < LPT / 2 ? a0 : a1), voff[c % (LPT / 2)], to + TILEB + c * 1024);
+    return (ok0 ? 1u : 0u) | (ok1 ? 2u : 0u);
+  };
+
+  // ---- operand addresses in slot 0 ----
+  uint32_t ka[FP8 ? D / 64 : NKS], va[NDB][2];
+#pragma unroll
+  for (int s = 0; s < (FP8 ? D / 64 : NKS); ++s) ka[s] = w * 32768 + j16 * ROWB + (((4 * s + g) ^ attn_swz_k<ROWB>(j16)) << 4);
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if constexpr (FP8) {  // eight rows of one column: 4 g .. 4 g + 3 of both halves
+        const int i = j16 >> 1, r = (i < 4 ? 0 : 16) + 4 * g + (i & 3);
+        va[db][e] = w * 32768 + TILEB + r * ROWB + ((db ^ attn_swz_k<ROWB>(r)) << 4) + ((j16 & 1) << 3);
+      } else {  // four rows, 4 g .. 4 g + 3 of half e
+        const int r = 16 * e + 4 * g + (j16 >> 2);
+        va[db][e] = w * 32768 + TILEB + r * ROWB + (((2 * db + ((j16 & 3) >> 1)) ^ attn_swz_v<ROWB>(r)) << 4) + ((j16 & 1) << 3);
+      }
+    }
+
+  bf16x8 q[NQ][NKS];
+  f32x4 o[NQ][NDB];
+  float m[NQ], l[NQ];
+  auto start = [&]() __attribute__((always_inline)) {  // the rows of cp's unit
+    const int hk = cp.unit / QG, first = (cp.unit - hk * QG) * 16 * NQ;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int h = first + 16 * i + j16;
+      const char* const src = (const char*)p.q + ((size_t)cp.b * p.Hq + (size_t)hk * G + h) * (D * 2);
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) {
+        const int f = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;  // (e4m3: a 16-byte read holds two steps)
+        q[i][s] = __builtin_bit_cast(bf16x8, h < G ? *(const u32x4*)(src + f * 2) : u32x4{0, 0, 0, 0});
+      }
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[i] = -__builtin_inff();
+      l[i] = 0.f;
+    }
+  };
+  const int kept = rows_kept(G);
+  auto finish = [&](bool whole, int part) __attribute__((always_inline)) {
+    const int hk = cp.unit / QG, first = (cp.unit - hk * QG) * 16 * NQ;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int r = 16 * i + j16;
+      const float sum = sum_rows(l[i]);
+      if (first + r >= G) continue;
+      if (whole) {
+        const size_t row = (size_t)cp.b * p.Hq + (size_t)hk * G + first + r;
+        const float inv = sum == 0.f ? 0.f : p.out_scale / sum;
+        char* const dst = (char*)p.o + row * (D * 2) + g * 8;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+          *(u32x2*)(dst + db * 32) = u32x2{attn_pack_bf16(o[i][db][0] * inv, o[i][db][1] * inv), attn_pack_bf16(o[i][db][2] * inv, o[i][db][3] * inv)};
+        if (g == 0) p.lse[row] = sum == 0.f ? -__builtin_inff() : (m[i] * p.scale_log2 + __builtin_amdgcn_logf(sum)) * kLn2;
+      } else {
+        float* const dst = (float*)p.ws + (size_t)(2 * worker + part) * partial_floats(kept, D);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) *(f32x4*)(dst + r * D + db * 16 + g * 4) = o[i][db];
+        if (g == 0) {
+          dst[kept * D + 2 * r] = m[i];
+          dst[kept * D + 2 * r + 1] = sum;
+        }
+      }
+    }
+  };
+
+  uint32_t have = 0;  // two bits for each tile in the ring: which halves have a page
+  const int ahead = min(n, RING);
+  start();
+  int began = cp.t;
+  for (int i = 0; i < ahead; ++i) {
+    have |= issue(i) << (2 * i);
+    if (i + 1 < n) {
+      advance(ld);
+      entries(ld);
+    }
+  }
+  int slot = 0, part = 0;
+  for (int i = 0; i < n; ++i) {
+    const int base = slot * (2 * TILEB), left = min(n - 1 - i, RING - 1);  // tiles requested behind this one
+    auto wait = [&](auto value) __attribute__((always_inline)) {
+      constexpr int V = decltype(value)::value;  // loads of this tile that may still be under way
+      switch (left) {
+        case 0: ATTN_WAIT_VMCNT(V); break;
+        case 1: ATTN_WAIT_VMCNT(2 * LPT * (RING > 1 ? 1 : 0) + V); break;
+        case 2: ATTN_WAIT_VMCNT(2 * LPT * (RING > 2 ? 2 : 0) + V); break;
+        case 3: ATTN_WAIT_VMCNT(2 * LPT * (RING > 3 ? 3 : 0) + V); break;
+        case 4: ATTN_WAIT_VMCNT(2 * LPT * (RING > 4 ? 4 : 0) + V); break;
+        case 5: ATTN_WAIT_VMCNT(2 * LPT * (RING > 5 ? 5 : 0) + V); break;
+        case 6: ATTN_WAIT_VMCNT(2 * LPT * (RING > 6 ? 6 : 0) + V); break;
+        default: ATTN_WAIT_VMCNT(2 * LPT * (RING > 7 ? 7 : 0) + V); break;
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    wait(std::integral_constant<int, LPT>{});
+
+    // visible rows of the tile's halves
+    const int keys = cp.len - (cp.t << 5);
+    const int n0 = have & 1 ? min(keys, 16) : 0, n1 = have & 2 ? min(max(keys - 16, 0), 16) : 0;
+    const bool hidden = n0 + n1 < 32;
+
+    f32x4 s[NQ][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      bf16x8 k[NKS];
+      if constexpr (FP8) {
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+          const u32x4 c = *(LDS_AS u32x4*)(smem + ka[x] + base + e * 16 * ROWB);
+          k[2 * x] = e4m3_to_bf16(c[0], c[1]);
+          k[2 * x + 1] = e4m3_to_bf16(c[2], c[3]);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < NKS; ++x) k[x] = __builtin_bit_cast(bf16x8, *(LDS_AS u32x4*)(smem + ka[x] + base + e * 16 * ROWB));
+      }
+#pragma unroll
+      for (int i2 = 0; i2 < NQ; ++i2) {
+        s[i2][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NKS; ++x) s[i2][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[x], q[i2][x], s[i2][e], 0, 0, 0);
+      }
+    }
+    if (hidden) {
+#pragma unroll
+      for (int i2 = 0; i2 < NQ; ++i2)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (4 * g + r >= (e ? n1 : n0)) s[i2][e][r] = -__builtin_inff();
+    }
+
+    // streaming softmax; differences are taken before they are scaled, so that scores near the type's lowest value do not overflow
+    bf16x8 pr[NQ];
+#pragma unroll
+    for (int i2 = 0; i2 < NQ; ++i2) {
+      float mx = s[i2][0][0];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[i2][x >> 2][x & 3]);
+      const float m_new = fmaxf(m[i2], max_rows(mx)), ref = m_new == -__builtin_inff() ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f((m[i2] - ref) * p.scale_log2);
+      if (__any(m_new != m[i2])) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) o[i2][db] *= alpha;
+        l[i2] *= alpha;
+      }
+      m[i2] = m_new;
+      float e[8], sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        e[x] = __builtin_amdgcn_exp2f((s[i2][x >> 2][x & 3] - ref) * p.scale_log2);
+        sum += e[x];
+      }
+      l[i2] += sum;  // (of the unrounded probabilities, this lane's keys)
+      // bf16 for the matrix cores: half a step of each probability, as in attn_fwd
+      pr[i2] = __builtin_bit_cast(bf16x8, u32x4{attn_pack_bf16(e[0], e[1]), attn_pack_bf16(e[2], e[3]), attn_pack_bf16(e[4], e[5]), attn_pack_bf16(e[6], e[7])});
+    }
+
+    wait(std::integral_constant<int, 0>{});
+    if (hidden) {  // 0 times what lies in a hidden row would be NaN where that is not finite
+#pragma unroll
+      for (int c = 0; c < LPT; ++c) {
+        const int r = (c % (LPT / 2)) * PIECE_ROWS + lane / NCH;
+        if (r >= (c < LPT / 2 ? n0 : n1)) *(LDS_AS u32x4*)(smem + w * 32768 + base + TILEB + c * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      bf16x8 v;
+      if constexpr (FP8) {
+        const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)(smem + va[db][0] + base));
+        v = e4m3_to_bf16((uint32_t)c[0], (uint32_t)c[1]);
+      } else {
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(smem + va[db][0] + base));
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(smem + va[db][1] + base));
+        v = __builtin_bit_cast(bf16x8, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
+      }
+#pragma unroll
+      for (int i2 = 0; i2 < NQ; ++i2) o[i2][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[i2], o[i2][db], 0, 0, 0);
+    }
+
+    // the slot is free once its last operand has arrived
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    have >>= 2;
+    if (i + RING < n) {
+      have |= issue(slot) << (2 * (RING - 1));
+      if (i + RING + 1 < n) {
+        advance(ld);
+        entries(ld);
+      }
+    }
+    slot = slot == RING - 1 ? 0 : slot + 1;
+
+    const bool last = cp.t + 1 == cp.nt;
+    if (last || i + 1 == n) {
+      const bool whole = last && began == 0;
+      finish(whole, part);
+      part = 1;
+      if (i + 1 < n) {
+        advance(cp);
+        start();
+        began = 0;
+      }
+    } else {
+      ++cp.t;
+    }
+  }
+}
+
+// Joins what the waves left of the (sequence, key head) pairs that more than one of them took, and writes the rows of sequences
+// without keys.  One wave per query row; WAVES of them share a row where there are few rows, each with many parts.
+template <int D, int WAVES>
+__global__ void __launch_bounds__(256) kv_join_kernel(const DecodeParams p, int NQ) {
+  constexpr int LPR = D / 4, PER = 64 / LPR;  // lanes of a row, parts a wave adds at once
+  __shared__ float so[4][D], sm[4], sl[4];
+  const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int row = WAVES == 1 ? blockIdx.x * 4 + w : blockIdx.x;
+  if (row >= p.B * p.Hq) return;  // (WAVES 1: no barrier follows)
+  const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG, kept = rows_kept(G);
+  const int b = row / p.Hq, hq = row - b * p.Hq, hk = hq / G, qg = (hq - hk * G) / (16 * NQ), r = hq - hk * G - qg * 16 * NQ;
+  const int len = visible_keys(p, scalar_load(p.lens, b));
+  const size_t out = (size_t)row * D;
+  if (len == 0) {
+    if (WAVES == 1 || w == 0) {
+      for (int i = lane; i < D / 2; i += 64) ((uint32_t*)p.o)[out / 2 + i] = 0;
+      if (lane == 0) p.lse[row] = -__builtin_inff();
+    }
+    return;
+  }
+  // tiles in front of the sequence, and all of them
+  unsigned long long mine = 0, front = 0;
+  for (int x = lane; x < p.B; x += 64) {
+    const int nt = tiles_of(visible_keys(p, p.lens[x]));
+    mine += nt;
+    if (x < b) front += nt;
+  }
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) {
+    mine += __shfl_xor(mine, k);
+    front += __shfl_xor(front, k);
+  }
+  const unsigned long long all = uniform(mine) * (unsigned)units, nt = tiles_of(len);
+  const unsigned long long first = uniform(front) * (unsigned)units + (unsigned long long)(hk * QG + qg) * nt, last = first + nt - 1;
+  const int w0 = uniform((int)((((first + 1) << kWorkersLog2) - 1) / all)), w1 = uniform((int)((((last + 1) << kWorkersLog2) - 1) / all));
+  if (w0 == w1) return;  // one wave took it all
+  const int part0 = ((all * w0) >> kWorkersLog2) < first ? 1 : 0;
+  const int stride = partial_floats(kept, D);
+  const float* const ws = (const float*)p.ws;
+
+  const int sub = lane / LPR, col = (lane % LPR) * 4;
+  float m = -__builtin_inff(), l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile
+  const bool sparse = all < kWorkers;
+  const int parts = sparse ? (int)nt : w1 - w0 + 1;
+  for (int i = (WAVES == 1 ? 0 : w * PER) + sub; i < parts; i += PER * WAVES) {
+    const int x = sparse ? (int)(((((uint32_t)first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all) : w0 + i;
+    const float* const src = ws + (size_t)(2 * x + (x == w0 ? part0 : 0)) * stride;
+    const f32x4 po = *(const f32x4*)(src + r * D + col);
+    const float pm = src[kept * D + 2 * r], pl = src[kept * D + 2 * r + 1];
+    const float m_new = fmaxf(m, pm), ref = m_new == -__builtin_inff() ? 0.f : m_new;
+    const float a = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2), c = __builtin_amdgcn_exp2f((pm - ref) * p.scale_log2);
+    o = o * a + po * c;
+    l = l * a + pl * c;
     m = m_new;
   }
-  for (int e = 0; e < E; ++e) so[w][lane + 64 * e] = o[e];
-  if (lane == 0) {
-    sm[w] = m;
-    sl[w] = l;
+  auto merge = [&](float om, float ol, const f32x4& oo) __attribute__((always_inline)) {
+    const float m_new = fmaxf(m, om), ref = m_new == -__builtin_inff() ? 0.f : m_new;
+    const float a = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2), c = __builtin_amdgcn_exp2f((om - ref) * p.scale_log2);
+    o = o * a + oo * c;
+    l = l * a + ol * c;
+    m = m_new;
+  };
+#pragma unroll
+  for (int k = LPR; k < 64; k *= 2) {
+    const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
+    f32x4 oo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) oo[i] = __shfl_xor(o[i], k);
+    merge(om, ol, oo);
   }
-  __syncthreads();
-  if (w != 0) return;
-  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  const float ref = m == -__builtin_inff() ? 0.f : m;
-  l = 0.f;
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int k = 0; k < kWaves; ++k) {
-    const float a = __builtin_amdgcn_exp2f((sm[k] - ref) * p.scale_log2);
-    l += sl[k] * a;
-    for (int e = 0; e < E; ++e) o[e] += so[k][lane + 64 * e] * a;
+  if constexpr (WAVES > 1) {
+    if (sub == 0) *(f32x4*)&so[w][col] = o;
+    if (lane == 0) {
+      sm[w] = m;
+      sl[w] = l;
+    }
+    __syncthreads();
+    if (w != 0) return;
+    for (int k = 1; k < 4; ++k) merge(sm[k], sl[k], *(const f32x4*)&so[k][col]);
   }
+  if (sub != 0) return;
   const float inv = l == 0.f ? 0.f : p.out_scale / l;
-  for (int e = 0; e < E; ++e) ((__bf16*)p.o)[(size_t)blockIdx.x * D + lane + 64 * e] = (__bf16)(o[e] * inv);
-  if (lane == 0) p.lse[blockIdx.x] = l == 0.f ? -__builtin_inff() : (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  *(u32x2*)((char*)p.o + (out + col) * 2) = u32x2{attn_pack_bf16(o[0] * inv, o[1] * inv), attn_pack_bf16(o[2] * inv, o[3] * inv)};
+  if (lane == 0) p.lse[row] = l == 0.f ? -__builtin_inff() : (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int D, bool FP8>
+void launch_decode(const DecodeParams& p, int nq, hipStream_t stream) {
+  constexpr int grid = kWorkers / kWaves;
+  if (nq == 1) kv_decode_kernel<D, FP8, 1><<<grid, kWaves * 64, 0, stream>>>(p);
+  else if (nq == 2) kv_decode_kernel<D, FP8, 2><<<grid, kWaves * 64, 0, stream>>>(p);
+  else kv_decode_kernel<D, FP8, 4><<<grid, kWaves * 64, 0, stream>>>(p);
+}
+
+template <int D>
+void launch_join(const DecodeParams& p, int nq, hipStream_t stream) {
+  const int rows = p.B * p.Hq;
+  if (rows <= 1024) kv_join_kernel<D, 4><<<rows, 256, 0, stream>>>(p, nq);
+  else kv_join_kernel<D, 1><<<(rows + 3) / 4, 256, 0, stream>>>(p, nq);
 }
 
 }  // namespace
 
 int kv_decode_launch(const DecodeParams& p, int d, bool fp8, hipStream_t stream) {
-  const int grid = p.B * p.Hq;
-  if (d == 128 && fp8) kv_decode_kernel<128, true><<<grid, kWaves * 64, 0, stream>>>(p);
-  else if (d == 128) kv_decode_kernel<128, false><<<grid, kWaves * 64, 0, stream>>>(p);
-  else if (fp8) kv_decode_kernel<64, true><<<grid, kWaves * 64, 0, stream>>>(p);
-  else kv_decode_kernel<64, false><<<grid, kWaves * 64, 0, stream>>>(p);
+  const int nq = blocks_for(p.Hq / p.Hkv);
+  if (d == 128 && fp8) launch_decode<128, true>(p, nq, stream);
+  else if (d == 128) launch_decode<128, false>(p, nq, stream);
+  else if (fp8) launch_decode<64, true>(p, nq, stream);
+  else launch_decode<64, false>(p, nq, stream);
+  if (hipGetLastError() != hipSuccess) return 1;
+  if (d == 128) launch_join<128>(p, nq, stream);
+  else launch_join<64>(p, nq, stream);
   return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
-long long kv_decode_bytes(int, int, int, int) { return 16; }
+long long kv_decode_bytes(int B, int Hq, int Hkv, int d) {
+  (void)B;
+  return 2ll * kWorkers * partial_floats(rows_kept(Hq / Hkv), d) * (long long)sizeof(float);
+}

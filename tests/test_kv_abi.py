@@ -195,6 +195,8 @@ def _all_calls():
             calls += [("kv_append", dict(rope, seq=P, pages=P, q=P, k_cache=P, v_cache=P, T=4, S=4, Hq=2, Hkv=1, d=d, W=2, page_size=16, num_pages=9, dtype=t)) for t in (0, 1)]
         calls += [("kv_decode", dict(q=P, k_cache=P, v_cache=P, pages=P, lens=P, o=P, lse=P, workspace=P, B=2, Hq=G * 2, Hkv=2, d=d, W=2, page_size=16, num_pages=9,
                                      scale=0.1, dtype=t)) for t in (0, 1) for G in (1, 5, 16, 17, 32, 33, 65)]
+        # (many rows: one wave joins a row)
+        calls += [("kv_decode", dict(calls[-1][1], B=1500, Hq=2, Hkv=1))]
     return calls
 
 
