@@ -15,6 +15,14 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kMostWorkgroups = 1 << 20;  // (a launch holds 2^32 threads)
 
+constexpr int kMostPartials = 1024;  // workgroups of a backward pass, each with its sums of the weights' gradients
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+// A wave takes kSpan groups of heads of a token, unless all groups can be taken by one wave each that start at once (4 waves on each of 1024
+// SIMDs): the smallest calls last as long as one wave's chain.  us at span 1 / 3 / 4 / 5 / 8: 16384 tokens of 64/8 heads, d = 128
+// 157 / 131 / 128 / 127 / 130; 10015 tokens of 32/8 heads into an e4m3 cache 57.6 / 45.3 / 45.0 / 46.2 / 47.9.
+constexpr int kSpan = 4, kFewTasks = 4096;
+
 // sum over the LPR (4 or 8) neighbouring lanes of a row, the same value in all of them
 template <int LPR>
 __device__ __forceinline__ float row_sum(float x) {
@@ -58,7 +66,6 @@ __device__ __forceinline__ void load_angles(const RopeParams& p, const Chunks& c
     sn[i] = 0.f;
   }
   if (!c.rotated) return;
-  typedef __attribute__((ext_vector_type(4))) float f32x4;
   const f32x4* const row = (const f32x4*)(p.table + (size_t)pos * p.rot);
   const int at0 = p.interleaved ? 2 * c.a : 4 * c.a, at1 = p.interleaved ? 2 * c.b : 4 * c.a + 2;
 #pragma unroll
@@ -122,82 +129,101 @@ __device__ __forceinline__ u32x2 to_e4m3(const float (&x)[8], float descale) {
 
 enum { kLayout = 0, kCacheBf16 = 1, kCacheFp8 = 2 };
 
-// 64 / (d / 16) consecutive heads of one token, by one wave
+// scalar load of what no kernel writes while this one runs
+__device__ __forceinline__ int scalar_load(const int* p, size_t i) { return ((const __attribute__((address_space(4))) int*)p)[i]; }
+
+// One task, by one wave: `span` groups of 64 / (d / 16) consecutive heads of one token.  The token's position, page and angles and the norms'
+// weights are fetched once for all of them, the rows of the next group while the ones of this group are computed.
 template <int D, int MODE>
-__device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int task) {
+__device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int span, int task) {
   constexpr int LPR = D / 16, RPW = 64 / LPR;
-  const int lane = threadIdx.x & 63;
-  const int t = task / groups, h = (task % groups) * RPW + lane / LPR, j = lane % LPR;
-  const int H = p.Hq + 2 * p.Hkv;
-  if (h >= H) return;
+  const int lane = threadIdx.x & 63, j = lane % LPR, H = p.Hq + 2 * p.Hkv;
+  const int spans = (groups + span - 1) / span, t = task / spans, g0 = (task - t * spans) * span, g1 = min(g0 + span, groups);
   const Chunks c = chunks_of<LPR>(j, p.rot);
 
-  int pos = p.pos ? p.pos[t] : t % (p.N > 0 ? p.N : 1);
-  int entry = -1, seq = 0;
+  const char* const row = (const char*)p.qkv + (size_t)t * p.ld * 2;
+  auto fetch = [&](int g, u32x4& xa, u32x4& xb) __attribute__((always_inline)) {
+    const char* const src = row + (size_t)min(g * RPW + lane / LPR, H - 1) * (D * 2);  // (heads past the last are not written)
+    xa = *(const u32x4*)(src + c.a * 16);
+    xb = *(const u32x4*)(src + c.b * 16);
+  };
+  u32x4 xa, xb, wq[2], wk[2];
+  fetch(g0, xa, xb);
+  if (p.wq) {
+    wq[0] = *(const u32x4*)((const char*)p.wq + c.a * 16);
+    wq[1] = *(const u32x4*)((const char*)p.wq + c.b * 16);
+    wk[0] = *(const u32x4*)((const char*)p.wk + c.a * 16);
+    wk[1] = *(const u32x4*)((const char*)p.wk + c.b * 16);
+  }
+
+  const int bb = MODE == kLayout ? t / p.N : 0, n = MODE == kLayout ? t - bb * p.N : 0;
+  const int pos = p.pos ? scalar_load(p.pos, t) : n;
+  int entry = -1;
   bool good = p.rot == 0 || (unsigned)pos < (unsigned)p.npos;
   if constexpr (MODE != kLayout) {
     if (pos < 0) return;  // padding
-    good = p.rot == 0 || pos < p.npos;
-    seq = p.seq ? p.seq[t] : t;
+    const int seq = p.seq ? scalar_load(p.seq, t) : t;
     good = good && (unsigned)seq < (unsigned)p.S;
-    if (good && (pos >> p.page_log2) < p.W) entry = p.pages[(size_t)seq * p.W + (pos >> p.page_log2)];
+    if (good && (pos >> p.page_log2) < p.W) entry = scalar_load(p.pages, (size_t)seq * p.W + (pos >> p.page_log2));
     if ((unsigned)entry >= (unsigned)p.num_pages) entry = -1;
   }
+  float cs[8], sn[8];
+  load_angles(p, c, good ? pos : 0, cs, sn);
 
-  const char* const src = (const char*)p.qkv + ((size_t)t * p.ld + (size_t)h * D) * 2;
-  const u32x4 xa = *(const u32x4*)(src + c.a * 16), xb = *(const u32x4*)(src + c.b * 16);
-  const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
-  float a[8], b[8];
-  unpack(xa, a);
-  unpack(xb, b);
-  if (!is_v) {
-    if (p.wq) {
-      const char* const wsrc = (const char*)(is_q ? p.wq : p.wk);
-      float wa[8], wb[8];
-      unpack(*(const u32x4*)(wsrc + c.a * 16), wa);
-      unpack(*(const u32x4*)(wsrc + c.b * 16), wb);
-      const float r = inverse_rms<LPR>(a, b, p.eps);
+  for (int g = g0; g < g1; ++g) {
+    const u32x4 ya = xa, yb = xb;
+    if (g + 1 < g1) fetch(g + 1, xa, xb);
+    const int h = g * RPW + lane / LPR;
+    if (h >= H) continue;
+    const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
+    float a[8], b[8];
+    unpack(ya, a);
+    unpack(yb, b);
+    if (!is_v) {
+      if (p.wq) {
+        float wa[8], wb[8];
+        unpack(is_q ? wq[0] : wk[0], wa);
+        unpack(is_q ? wq[1] : wk[1], wb);
+        const float r = inverse_rms<LPR>(a, b, p.eps);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        a[i] = a[i] * r * wa[i];
-        b[i] = b[i] * r * wb[i];
+        for (int i = 0; i < 8; ++i) {
+          a[i] = a[i] * r * wa[i];
+          b[i] = b[i] * r * wb[i];
+        }
+      }
+      rotate<1>(p.interleaved, a, b, cs, sn);
+      if (!good) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
       }
     }
-    float cs[8], sn[8];
-    load_angles(p, c, good ? pos : 0, cs, sn);
-    rotate<1>(p.interleaved, a, b, cs, sn);
-    if (!good) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
+    const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
+    char* dst;
+    if constexpr (MODE == kLayout) {
+      const int Hk = is_q ? p.Hq : p.Hkv;
+      dst = (char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
+    } else if (is_q) {
+      dst = (char*)p.q + ((size_t)t * p.Hq + hk) * (D * 2);
+    } else {
+      if (!good || entry < 0) continue;
+      const size_t place = (((size_t)entry * p.Hkv + hk) << p.page_log2) + (pos & ((1 << p.page_log2) - 1));
+      dst = (char*)(is_v ? p.v : p.k) + place * (D * (MODE == kCacheFp8 ? 1 : 2));
+      if constexpr (MODE == kCacheFp8) {
+        const float descale = is_v ? p.v_descale : p.k_descale;
+        *(u32x2*)(dst + c.a * 8) = to_e4m3(a, descale);
+        *(u32x2*)(dst + c.b * 8) = to_e4m3(b, descale);
+        continue;
+      }
     }
+    *(u32x4*)(dst + c.a * 16) = is_v ? ya : pack(a);
+    *(u32x4*)(dst + c.b * 16) = is_v ? yb : pack(b);
   }
-
-  const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
-  char* dst;
-  if constexpr (MODE == kLayout) {
-    const int n = t % p.N, bb = t / p.N, Hk = is_q ? p.Hq : p.Hkv;
-    dst = (char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
-  } else if (is_q) {
-    dst = (char*)p.q + ((size_t)t * p.Hq + hk) * (D * 2);
-  } else {
-    if (!good || entry < 0) return;
-    const size_t row = (((size_t)entry * p.Hkv + hk) << p.page_log2) + (pos & ((1 << p.page_log2) - 1));
-    dst = (char*)(is_v ? p.v : p.k) + row * (D * (MODE == kCacheFp8 ? 1 : 2));
-    if constexpr (MODE == kCacheFp8) {
-      const float descale = is_v ? p.v_descale : p.k_descale;
-      *(u32x2*)(dst + c.a * 8) = to_e4m3(a, descale);
-      *(u32x2*)(dst + c.b * 8) = to_e4m3(b, descale);
-      return;
-    }
-  }
-  *(u32x4*)(dst + c.a * 16) = is_v ? xa : pack(a);
-  *(u32x4*)(dst + c.b * 16) = is_v ? xb : pack(b);
 }
 
 template <int D, int MODE>
-__global__ void __launch_bounds__(kWaves * 64) rope_qkv_kernel(const RopeParams p, int groups, int tasks) {
+__global__ void __launch_bounds__(kWaves * 64) rope_qkv_kernel(const RopeParams p, int groups, int span, int tasks) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) rope_task<D, MODE>(p, groups, task);
+  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) rope_task<D, MODE>(p, groups, span, task);
 }
 
 // The gradients.  A workgroup walks tasks (a token's 64 / (d / 16) heads) a grid apart and keeps what its lanes add to the
@@ -272,43 +298,58 @@ __global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopePar
   }
 
   if constexpr (NORM) {
-    // over the rows a wave holds at once (lanes that agree mod LPR), then over the waves
-    __shared__ float part[kWaves][2][D];
+    // over the rows that the lanes held (those that agree mod LPR) and the waves, through LDS: a column is the sum of 64 / LPR * kWaves
+    // values, taken by two (d = 64) or one of the threads.  (By exchanges between lanes: 128 of them at d = 64, 2 us.)
+    constexpr int PITCH = 2 * D + 4;  // floats of a row of sums: q's d, k's d
+    __shared__ __attribute__((aligned(16))) float part[kWaves * RPW][PITCH];
+    float* const mine = part[w * RPW + lane / LPR];
 #pragma unroll
     for (int qk = 0; qk < 2; ++qk)
 #pragma unroll
       for (int ab = 0; ab < 2; ++ab)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float x = acc[qk][ab][i];
-#pragma unroll
-          for (int m = LPR; m < 64; m *= 2) x += __shfl_xor(x, m);
-          if (lane < LPR) part[w][qk][(ab ? c.b : c.a) * 8 + i] = x;
-        }
+        for (int i = 0; i < 8; i += 4)
+          *(f32x4*)(mine + qk * D + (ab ? c.b : c.a) * 8 + i) = f32x4{acc[qk][ab][i], acc[qk][ab][i + 1], acc[qk][ab][i + 2], acc[qk][ab][i + 3]};
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * D; i += kWaves * 64) {
-      float x = 0.f;
+    constexpr int SHARE = kWaves * 64 / (2 * D);  // threads of a column
+    const int col = threadIdx.x % (2 * D), at = threadIdx.x / (2 * D);
+    float x = 0.f;
 #pragma unroll
-      for (int k = 0; k < kWaves; ++k) x += part[k][i / D][i % D];
-      p.partial[(size_t)blockIdx.x * (2 * D) + i] = x;
+    for (int i = 0; i < kWaves * RPW / SHARE; ++i) x += part[i * SHARE + at][col];
+    if constexpr (SHARE == 2) {
+      __syncthreads();
+      part[at][col] = x;
+      __syncthreads();
+      x = part[0][col] + part[1][col];
     }
+    if (at == 0) p.partial[(size_t)blockIdx.x * (2 * D) + col] = x;
   }
 }
 
-// the sums over workgroups: one workgroup for 16 of the 2 d columns, 16 threads each
+// the sums over workgroups: one workgroup for 16 of the 2 d columns; four threads take their four columns of a row each, so that at most
+// four loads of every thread are under way at once
 template <int D>
-__global__ void __launch_bounds__(256) rope_weight_sum_kernel(const float* partial, int workgroups, float* dwq, float* dwk) {
-  __shared__ float part[16][16];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), at = threadIdx.x >> 4;
-  float x = 0.f;
-  for (int i = at; i < workgroups; i += 16) x += partial[(size_t)i * (2 * D) + col];
-  part[at][threadIdx.x & 15] = x;
-  __syncthreads();
-  if (at == 0) {
-    x = 0.f;
+__global__ void __launch_bounds__(1024) rope_weight_sum_kernel(const float* partial, int workgroups, float* dwq, float* dwk) {
+  __shared__ f32x4 part[16][4];
+  const int c4 = threadIdx.x & 3, at = threadIdx.x >> 2, w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const float* const src = partial + blockIdx.x * 16 + c4 * 4;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x += part[i][threadIdx.x];
-    (col < D ? dwq : dwk)[col % D] = x;
+  for (int i = 0; i < kMostPartials / 256; ++i)
+    if (i * 256 + at < workgroups) x += *(const f32x4*)(src + (size_t)(i * 256 + at) * (2 * D));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int m = 4; m < 64; m *= 2) x[i] += __shfl_xor(x[i], m);
+  }
+  if (lane < 4) part[w][lane] = x;
+  __syncthreads();
+  if (threadIdx.x < 16) {
+    const int col = blockIdx.x * 16 + threadIdx.x;
+    float y = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y += part[i][threadIdx.x >> 2][threadIdx.x & 3];
+    (col < D ? dwq : dwk)[col % D] = y;
   }
 }
 
@@ -323,9 +364,10 @@ int tasks_of(const RopeParams& p, int d, int* groups) {
 template <int MODE>
 int launch_rows(const RopeParams& p, int d, hipStream_t stream) {
   int groups;
-  const int tasks = tasks_of(p, d, &groups), grid = min((tasks - 1) / kWaves + 1, kMostWorkgroups);
-  if (d == 128) rope_qkv_kernel<128, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
-  else rope_qkv_kernel<64, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
+  const int all = tasks_of(p, d, &groups), span = all <= kFewTasks ? 1 : kSpan;
+  const int tasks = p.T * ((groups + span - 1) / span), grid = min((tasks - 1) / kWaves + 1, kMostWorkgroups);
+  if (d == 128) rope_qkv_kernel<128, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
+  else rope_qkv_kernel<64, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
   return launched();
 }
 
@@ -339,7 +381,7 @@ int kv_append_launch(const RopeParams& p, int d, bool fp8, hipStream_t stream) {
 
 int rope_qkv_bwd_workgroups(long long T, long long heads, int d) {
   const long long rows = d >= 1024 ? 1 : 1024 / d, tasks = T * ((heads + rows - 1) / rows), wgs = (tasks + kWaves - 1) / kWaves;
-  return (int)(wgs < 1024 ? wgs : 1024);
+  return (int)(wgs < kMostPartials ? wgs : kMostPartials);
 }
 
 int rope_qkv_bwd_launch(const RopeParams& p, int d, hipStream_t stream) {
@@ -349,8 +391,8 @@ int rope_qkv_bwd_launch(const RopeParams& p, int d, hipStream_t stream) {
     if (d == 128) rope_qkv_bwd_kernel<128, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
     else rope_qkv_bwd_kernel<64, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
     if (launched() != 0) return 1;
-    if (d == 128) rope_weight_sum_kernel<128><<<2 * 128 / 16, 256, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
-    else rope_weight_sum_kernel<64><<<2 * 64 / 16, 256, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
+    if (d == 128) rope_weight_sum_kernel<128><<<2 * 128 / 16, 1024, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
+    else rope_weight_sum_kernel<64><<<2 * 64 / 16, 1024, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
   } else {
     if (d == 128) rope_qkv_bwd_kernel<128, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
     else rope_qkv_bwd_kernel<64, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);

@@ -1,13 +1,16 @@
 """ctypes binding of include/kv.h: same names, argument marshalling only.
 
-Beside device addresses the calls take torch tensors, whose type, device and layout are checked: a mistake there would
+Beside device addresses the calls take torch tensors, whose type, device, layout and size are checked: a mistake there would
 otherwise be read as other numbers, or past the end, by the GPU."""
 from __future__ import annotations
 
 import ctypes as C
 import os
 
-from .binding import HERE, AttnError, _stream
+import torch
+
+from .binding import HERE, AttnError
+from .binding import _stream as _stream_of
 
 lib_path = os.path.join(HERE, "libkv_mi355x.so")
 
@@ -37,78 +40,79 @@ lib.kv_decode.restype = _i
 lib.kv_decode_workspace_bytes.argtypes = [_i] * 4
 lib.kv_decode_workspace_bytes.restype = _ll
 
-
-def _types():
-    import torch
-
-    # (torch is imported when the first tensor comes: the library itself needs none of it)
-    global _BF16, _F32, _I32, _U8
-    _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, (torch.uint8, torch.float8_e4m3fn)
-    return torch
+_BF16, _F32, _I32, _U8, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
 
 
-_BF16 = _F32 = _I32 = _U8 = None
-_KINDS = {"bf16": lambda: (_BF16,), "f32": lambda: (_F32,), "i32": lambda: (_I32,), "e4m3": lambda: _U8}
+def _device():
+    """The current device; -1 (no tensor's) where there is none."""
+    try:
+        return torch._C._cuda_getDevice()  # (torch.cuda.current_device without 150 ns of Python)
+    except AttributeError:
+        return torch.cuda.current_device()
+    except RuntimeError:
+        return -1
 
 
-class _Args:
-    """Device pointers of the tensors of one call; all of them on the current device."""
+def _stream(stream, device):
+    if stream is None:
+        try:
+            return torch._C._cuda_getCurrentRawStream(device)  # (the handle alone, as the other calls take it)
+        except (AttributeError, RuntimeError):
+            pass
+    return _stream_of(stream)
 
-    __slots__ = ("call", "device")
 
-    def __init__(self, call):
-        self.call, self.device = call, None
-
-    def _checked(self, t, kind, name):
-        if _BF16 is None:
-            _types()
-        if t.dtype not in _KINDS[kind]():
-            raise ValueError(f"{self.call}: {name} is {t.dtype}, not {kind}")
-        device = t.get_device()
-        if device != self.device:
-            if device < 0:
-                raise ValueError(f"{self.call}: {name} is not on a GPU")
-            import torch
-
-            self.device = torch.cuda.current_device()
-            if device != self.device:
-                raise ValueError(f"{self.call}: {name} is on device {device}, the current one is {self.device}")
-        return t.data_ptr()
-
-    def __call__(self, t, kind, name, least=0):
-        """`least`: the number of elements that the call reads or writes."""
+# A small call takes as long as the host takes for it, so a tensor's checks are one expression: 0.25 us each, ten of them in kv_append.
+def _ptr(t, dtype, least, device, name):
+    """Address of a tensor of at least `least` elements (what the call reads or writes), or of what is an address already."""
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() >= least and device >= 0:
+            return t.data_ptr()
+    except AttributeError:
         if t is None or isinstance(t, int):
             return t
-        ptr = self._checked(t, kind, name)
-        if not t.is_contiguous():
-            raise ValueError(f"{self.call}: {name} must be contiguous")
-        if t.numel() < least:
-            raise ValueError(f"{self.call}: {name} has {t.numel()} elements, {least} are needed")
-        return ptr
+        raise TypeError(f"{name} is {type(t).__name__}, not a tensor or an address") from None
+    _refuse_other(t, dtype, device, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} has {t.numel()} elements, {least} are needed")
 
-    def rows(self, t, ld, rows, width, name):
-        """`rows` rows of `width` features, `ld` elements apart."""
+
+def _refuse_other(t, dtype, device, name):
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    if t.get_device() < 0:
+        raise ValueError(f"{name} is not on a GPU")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current one is {device}")
+
+
+def _rows(t, ld, rows, width, device, name):
+    """Address of `rows` rows of `width` bf16 features, `ld` elements apart."""
+    try:
+        if t.dtype is _BF16 and t.get_device() == device and t.is_contiguous() and t.numel() >= (rows - 1) * ld + width and device >= 0:
+            return t.data_ptr()  # (a dense buffer may be given in any shape)
+    except AttributeError:
         if t is None or isinstance(t, int):
             return t
-        ptr = self._checked(t, "bf16", name)
-        shape, stride, step = t.shape, t.stride(), ld
-        ok = len(shape) > 0 and (shape[-1] == 1 or stride[-1] == 1)
-        if t.is_contiguous():  # (a dense buffer may be given in any shape)
-            ok = t.numel() >= (rows - 1) * ld + width
-        else:
-            count = 1
-            for n, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
-                ok = ok and (n == 1 or s == step)
-                step *= n
-                count *= n
-            ok = ok and count >= rows and shape[-1] >= width
-        if not ok:
-            raise ValueError(f"{self.call}: {name} (shape {tuple(shape)}, strides {tuple(stride)}) does not hold {rows} rows of {width}, {ld} apart")
-        return ptr
+        raise TypeError(f"{name} is {type(t).__name__}, not a tensor or an address") from None
+    _refuse_other(t, _BF16, device, name)
+    shape, stride = t.shape, t.stride()
+    ok = not t.is_contiguous() and shape[-1] >= width and stride[-1] == 1
+    step, count = ld, 1
+    for n, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        ok = ok and (n == 1 or s == step)
+        step *= n
+        count *= n
+    if not ok or count < rows:
+        raise ValueError(f"{name} (shape {tuple(shape)}, strides {tuple(stride)}) does not hold {rows} rows of {width}, {ld} apart")
+    return t.data_ptr()
 
 
-def _rope_args(a, q_weight, k_weight, table, npos, rot, pos, T, d):
-    return (a(q_weight, "bf16", "q_weight", d), a(k_weight, "bf16", "k_weight", d), a(table, "f32", "table", npos * rot), a(pos, "i32", "pos", T))
+def _cache(t, dtype, least, device, name):
+    """e4m3 caches are bytes, or torch's type of them."""
+    kind = _BF16 if dtype != 1 else _E4M3 if getattr(t, "dtype", None) is _E4M3 else _U8
+    return _ptr(t, kind, least, device, name)
 
 
 def _done(st, check, call):
@@ -118,10 +122,11 @@ def _done(st, check, call):
 
 
 def rope_qkv(qkv, ld, q_weight, k_weight, eps, table, npos, rot, interleaved, pos, q, k, v, B, Hq, Hkv, N, d, stream=None, check=True):
-    a, T = _Args("rope_qkv"), B * N
-    wq, wk, tab, ps = _rope_args(a, q_weight, k_weight, table, npos, rot, pos, T, d)
-    st = lib.rope_qkv(a.rows(qkv, ld, T, (Hq + 2 * Hkv) * d, "qkv"), ld, wq, wk, eps, tab, npos, rot, 1 if interleaved else 0, ps,
-                      a(q, "bf16", "q", T * Hq * d), a(k, "bf16", "k", T * Hkv * d), a(v, "bf16", "v", T * Hkv * d), B, Hq, Hkv, N, d, _stream(stream))
+    D, T = _device(), B * N
+    nk = T * Hkv * d
+    st = lib.rope_qkv(_rows(qkv, ld, T, (Hq + 2 * Hkv) * d, D, "qkv"), ld, _ptr(q_weight, _BF16, d, D, "q_weight"), _ptr(k_weight, _BF16, d, D, "k_weight"), eps,
+                      _ptr(table, _F32, npos * rot, D, "table"), npos, rot, 1 if interleaved else 0, _ptr(pos, _I32, T, D, "pos"),
+                      _ptr(q, _BF16, T * Hq * d, D, "q"), _ptr(k, _BF16, nk, D, "k"), _ptr(v, _BF16, nk, D, "v"), B, Hq, Hkv, N, d, _stream(stream, D))
     return _done(st, check, "rope_qkv")
 
 
@@ -131,24 +136,22 @@ def rope_qkv_bwd_workspace_bytes(B: int, Hq: int, Hkv: int, N: int, d: int) -> i
 
 def rope_qkv_bwd(dq, dk, dv, qkv, ld, q_weight, k_weight, eps, table, npos, rot, interleaved, pos, dqkv, dld, dq_weight, dk_weight, workspace,
                  B, Hq, Hkv, N, d, stream=None, check=True):
-    a, T, width = _Args("rope_qkv_bwd"), B * N, (Hq + 2 * Hkv) * d
-    wq, wk, tab, ps = _rope_args(a, q_weight, k_weight, table, npos, rot, pos, T, d)
-    need = rope_qkv_bwd_workspace_bytes(B, Hq, Hkv, N, d) // 4 if q_weight is not None else 0
-    st = lib.rope_qkv_bwd(a(dq, "bf16", "dq", T * Hq * d), a(dk, "bf16", "dk", T * Hkv * d), a(dv, "bf16", "dv", T * Hkv * d),
-                          a.rows(qkv, ld, T, width, "qkv"), ld, wq, wk, eps, tab, npos, rot, 1 if interleaved else 0, ps,
-                          a.rows(dqkv, dld, T, width, "dqkv"), dld, a(dq_weight, "f32", "dq_weight", d), a(dk_weight, "f32", "dk_weight", d),
-                          a(workspace, "f32", "workspace", need), B, Hq, Hkv, N, d, _stream(stream))
+    D, T, width = _device(), B * N, (Hq + 2 * Hkv) * d
+    nk, need = T * Hkv * d, lib.rope_qkv_bwd_workspace_bytes(B, Hq, Hkv, N, d) // 4
+    st = lib.rope_qkv_bwd(_ptr(dq, _BF16, T * Hq * d, D, "dq"), _ptr(dk, _BF16, nk, D, "dk"), _ptr(dv, _BF16, nk, D, "dv"), _rows(qkv, ld, T, width, D, "qkv"), ld,
+                          _ptr(q_weight, _BF16, d, D, "q_weight"), _ptr(k_weight, _BF16, d, D, "k_weight"), eps, _ptr(table, _F32, npos * rot, D, "table"), npos, rot,
+                          1 if interleaved else 0, _ptr(pos, _I32, T, D, "pos"), _rows(dqkv, dld, T, width, D, "dqkv"), dld, _ptr(dq_weight, _F32, d, D, "dq_weight"),
+                          _ptr(dk_weight, _F32, d, D, "dk_weight"), _ptr(workspace, _F32, need, D, "workspace"), B, Hq, Hkv, N, d, _stream(stream, D))
     return _done(st, check, "rope_qkv_bwd")
 
 
 def kv_append(qkv, ld, q_weight, k_weight, eps, table, npos, rot, interleaved, pos, seq, pages, q, k_cache, v_cache, T, S, Hq, Hkv, d,
               W, page_size, num_pages, dtype, k_descale=1.0, v_descale=1.0, stream=None, check=True):
-    a, held, kind = _Args("kv_append"), num_pages * Hkv * page_size * d, "e4m3" if dtype == 1 else "bf16"
-    wq, wk, tab, ps = _rope_args(a, q_weight, k_weight, table, npos, rot, pos, T, d)
-    st = lib.kv_append(a.rows(qkv, ld, T, (Hq + 2 * Hkv) * d, "qkv"), ld, wq, wk, eps, tab, npos, rot, 1 if interleaved else 0, ps,
-                       a(seq, "i32", "seq", T), a(pages, "i32", "pages", S * W), a(q, "bf16", "q", T * Hq * d),
-                       a(k_cache, kind, "k_cache", held), a(v_cache, kind, "v_cache", held), T, S, Hq, Hkv, d, W, page_size, num_pages,
-                       dtype, k_descale, v_descale, _stream(stream))
+    D, held = _device(), num_pages * Hkv * page_size * d
+    st = lib.kv_append(_rows(qkv, ld, T, (Hq + 2 * Hkv) * d, D, "qkv"), ld, _ptr(q_weight, _BF16, d, D, "q_weight"), _ptr(k_weight, _BF16, d, D, "k_weight"), eps,
+                       _ptr(table, _F32, npos * rot, D, "table"), npos, rot, 1 if interleaved else 0, _ptr(pos, _I32, T, D, "pos"), _ptr(seq, _I32, T, D, "seq"),
+                       _ptr(pages, _I32, S * W, D, "pages"), _ptr(q, _BF16, T * Hq * d, D, "q"), _cache(k_cache, dtype, held, D, "k_cache"),
+                       _cache(v_cache, dtype, held, D, "v_cache"), T, S, Hq, Hkv, d, W, page_size, num_pages, dtype, k_descale, v_descale, _stream(stream, D))
     return _done(st, check, "kv_append")
 
 
@@ -158,9 +161,9 @@ def kv_decode_workspace_bytes(B: int, Hq: int, Hkv: int, d: int) -> int:
 
 def kv_decode(q, k_cache, v_cache, pages, lens, o, lse, workspace, B, Hq, Hkv, d, W, page_size, num_pages, scale, dtype, k_descale=1.0,
               v_descale=1.0, stream=None, check=True):
-    a, held, kind = _Args("kv_decode"), num_pages * Hkv * page_size * d, "e4m3" if dtype == 1 else "bf16"
-    st = lib.kv_decode(a(q, "bf16", "q", B * Hq * d), a(k_cache, kind, "k_cache", held), a(v_cache, kind, "v_cache", held),
-                       a(pages, "i32", "pages", B * W), a(lens, "i32", "lens", B), a(o, "bf16", "o", B * Hq * d), a(lse, "f32", "lse", B * Hq),
-                       a(workspace, "f32", "workspace", lib.kv_decode_workspace_bytes(B, Hq, Hkv, d) // 4), B, Hq, Hkv, d, W, page_size, num_pages,
-                       scale, dtype, k_descale, v_descale, _stream(stream))
+    D, held, nq = _device(), num_pages * Hkv * page_size * d, B * Hq * d
+    need = lib.kv_decode_workspace_bytes(B, Hq, Hkv, d) // 4
+    st = lib.kv_decode(_ptr(q, _BF16, nq, D, "q"), _cache(k_cache, dtype, held, D, "k_cache"), _cache(v_cache, dtype, held, D, "v_cache"),
+                       _ptr(pages, _I32, B * W, D, "pages"), _ptr(lens, _I32, B, D, "lens"), _ptr(o, _BF16, nq, D, "o"), _ptr(lse, _F32, B * Hq, D, "lse"),
+                       _ptr(workspace, _F32, need, D, "workspace"), B, Hq, Hkv, d, W, page_size, num_pages, scale, dtype, k_descale, v_descale, _stream(stream, D))
     return _done(st, check, "kv_decode")

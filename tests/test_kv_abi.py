@@ -110,8 +110,9 @@ def test_workspace_sizes(A):
 def test_tensors_that_the_gpu_could_not_read_are_refused(A):
     """Other types, CPU tensors, strides and too few elements are errors of the binding, before the library is called."""
     bf, i32 = torch.zeros(4096, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.int32)
-    for kw, text in ((dict(q=bf.float()), "not bf16"), (dict(q=bf), "not on a GPU"), (dict(lens=i32.long()), "not i32"), (dict(lens=i32), "not on a GPU"),
-                     (dict(k_cache=bf, dtype=1), "not e4m3"), (dict(workspace=bf), "not f32")):
+    for kw, text in ((dict(q=bf.float()), "q is torch.float32"), (dict(q=bf), "q is not on a GPU"), (dict(lens=i32.long()), "lens is torch.int64"),
+                     (dict(lens=i32), "not on a GPU"), (dict(k_cache=bf, dtype=1), "k_cache is torch.bfloat16"), (dict(workspace=bf), "not torch.float32"),
+                     (dict(v_cache=bf.view(torch.uint8)), "v_cache is torch.uint8")):
         with pytest.raises(ValueError, match=text):
             _decode(A, **kw)
     for call, kw in ((_rope, dict(qkv=bf)), (_rope, dict(pos=i32.float())), (_bwd, dict(dqkv=bf)), (_append, dict(seq=i32)), (_append, dict(v_cache=i32))):
@@ -120,43 +121,45 @@ def test_tensors_that_the_gpu_could_not_read_are_refused(A):
 
 
 class _Fake:
-    """What the binding asks of a tensor on the current device."""
+    """What the binding asks of a tensor on device 0."""
 
-    def __init__(self, t):
-        self.t, self.dtype, self.shape = t, t.dtype, t.shape
+    def __init__(self, t, device=0):
+        self.t, self.dtype, self.shape, self.device = t, t.dtype, t.shape, device
 
     def __getattr__(self, name):
         return getattr(self.t, name)
 
     def get_device(self):
-        return 0
+        return self.device
 
 
-def test_layouts_are_checked(monkeypatch):
+def test_layouts_are_checked():
     kv = importlib.import_module("paper_2605_10905_amd.kv")
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    a = kv._Args("call")
-    x = torch.zeros(6, 40, dtype=torch.bfloat16)
-    assert a(_Fake(x), "bf16", "x", 240) == x.data_ptr()
+    bf = torch.bfloat16
+    x = torch.zeros(6, 40, dtype=bf)
+    assert kv._ptr(_Fake(x), bf, 240, 0, "x") == x.data_ptr() and kv._ptr(None, bf, 1, 0, "x") is None and kv._ptr(64, bf, 1, 0, "x") == 64
     with pytest.raises(ValueError, match="240 elements, 241"):
-        a(_Fake(x), "bf16", "x", 241)
+        kv._ptr(_Fake(x), bf, 241, 0, "x")
     with pytest.raises(ValueError, match="contiguous"):
-        a(_Fake(x.t()), "bf16", "x", 1)
-    assert a.rows(_Fake(x), 40, 6, 40, "x") and a.rows(_Fake(x[:, :32]), 40, 6, 32, "x") and a.rows(_Fake(x.view(2, 3, 40)[:, :, 8:]), 40, 6, 32, "x")
-    assert a.rows(_Fake(x.view(-1)), 40, 6, 40, "x") and a.rows(_Fake(x[:1, :32]), 40, 1, 32, "x")
+        kv._ptr(_Fake(x.t()), bf, 1, 0, "x")
+    with pytest.raises(ValueError, match="device 1, the current one is 0"):
+        kv._ptr(_Fake(x, 1), bf, 1, 0, "x")
+    with pytest.raises(ValueError, match="device 1, the current one is 0"):
+        kv._rows(_Fake(x, 1), 40, 6, 40, 0, "x")
+    with pytest.raises(TypeError, match="list"):
+        kv._ptr([1.0], bf, 1, 0, "x")
+    for t, ld, rows, width in ((x, 40, 6, 40), (x[:, :32], 40, 6, 32), (x.view(2, 3, 40)[:, :, 8:], 40, 6, 32), (x.view(-1), 40, 6, 40), (x[:2, :32], 40, 1, 32),
+                               (x[1:5, :32], 40, 4, 24)):
+        assert kv._rows(_Fake(t), ld, rows, width, 0, "x") == t.data_ptr()
     for t, ld, rows, width in ((x, 48, 6, 40), (x, 40, 7, 40), (x[:, :32], 40, 6, 40), (x[::2, :32], 40, 3, 32), (x[:, ::2], 40, 6, 20), (x.t(), 6, 40, 6),
                                (x.view(2, 3, 40)[:, :2], 40, 4, 40), (x[:, :32], 32, 6, 32)):
         with pytest.raises(ValueError, match="does not hold"):
-            a.rows(_Fake(t), ld, rows, width, "x")
-    b = kv._Args("call")
-    other = _Fake(x)
-    other.get_device = lambda: 1
-    with pytest.raises(ValueError, match="device 1, the current one is 0"):
-        b(other, "bf16", "x")
+            kv._rows(_Fake(t), ld, rows, width, 0, "x")
 
 
 _MAIN = """
 import ctypes, json, sys
+import torch  # (its own kernels are not ours to write down)
 rec = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
 rec.recorder_take.restype = rec.recorder_kernels.restype = ctypes.c_char_p
 sys.path.insert(0, sys.argv[2])
