@@ -41,49 +41,56 @@ __device__ __forceinline__ int scalar_load(const int* p, size_t i) { return ((co
 __device__ __forceinline__ int visible_keys(const DecodeParams& p, int len) { return min(max(len, 0), p.W << p.page_log2); }
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + 31) >> 5; }
 
-// All tiles of one key head: the sum over the sequences.
-__device__ __forceinline__ unsigned long long count_tiles(const DecodeParams& p) {
-  const int lane = threadIdx.x & 63;
-  unsigned long long mine = 0;
-  for (int b = lane; b < p.B; b += 64) mine += tiles_of(visible_keys(p, p.lens[b]));
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) mine += __shfl_xor(mine, m);
-  return uniform(mine);
-}
-
-// Tiles of one key head in front of every sequence of the 64 from `first` on (lane by lane), given those in front of `first`; their
-// sum fits 32 bits (2^25 tiles a sequence).
+// inclusive sums over the lanes: shifts inside rows of 16, then the rows' last sums
 __device__ __forceinline__ uint32_t scan64(uint32_t x) {
-  const int lane = threadIdx.x & 63;
-  uint32_t sum = x;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const uint32_t y = __shfl_up(sum, m);
-    if (lane >= m) sum += y;
-  }
-  return sum;
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);  // row_bcast 15 into rows 1 and 3
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);  // row_bcast 31 into rows 2 and 3
+  return x;
 }
 
-struct Place {
+// A wave's piece [begin, end) of the list of all tiles, and the sequence that it begins in.
+struct Piece {
+  unsigned long long all, begin, end;
   int b, len;                 // the sequence and its visible keys
   unsigned long long before;  // tiles of one key head in front of it
 };
-// The sequence that tile `at` of the list (units x tiles of each sequence) belongs to.
-__device__ __forceinline__ Place place_of(const DecodeParams& p, unsigned long long at, int units) {
+__device__ __forceinline__ Piece piece_of(const DecodeParams& p, int worker, int units) {
   const int lane = threadIdx.x & 63;
-  Place r = {0, 0, 0};
+  Piece r;
+  // (a sequence has at most 2^25 tiles: sums over 64 of them fit 32 bits)
+  int len = lane < p.B ? visible_keys(p, p.lens[lane]) : 0;
+  uint32_t own = tiles_of(len), incl = scan64(own);
+  unsigned long long total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+  if (p.B > 64) {
+    unsigned long long mine = 0;
+    for (int b = 64 + lane; b < p.B; b += 64) mine += tiles_of(visible_keys(p, p.lens[b]));
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) mine += __shfl_xor(mine, m);
+    total += uniform(mine);
+  }
+  r.all = total * (unsigned)units;
+  r.begin = (r.all * worker) >> kWorkersLog2;
+  r.end = (r.all * (worker + 1)) >> kWorkersLog2;
+  r.b = r.len = 0;
+  r.before = 0;
   unsigned long long base = 0;
-  for (int first = 0; first < p.B; first += 64) {
-    const int len = first + lane < p.B ? visible_keys(p, p.lens[first + lane]) : 0;
-    const uint32_t own = tiles_of(len), incl = scan64(own);
-    const unsigned long long before = base + (incl - own);
-    const int n = __popcll(__ballot(first + lane < p.B && before * (unsigned)units <= at));
+  for (int first = 0;;) {
+    const uint32_t excl = incl - own;
+    const int n = __popcll(__ballot(first + lane < p.B && (base + excl) * (unsigned)units <= r.begin));
     if (n == 0) break;
     r.b = first + n - 1;
     r.len = __builtin_amdgcn_readlane(len, n - 1);
-    r.before = base + (uint32_t)__builtin_amdgcn_readlane((int)(incl - own), n - 1);
-    if (n < 64) break;
+    r.before = base + (uint32_t)__builtin_amdgcn_readlane((int)excl, n - 1);
+    first += 64;
+    if (n < 64 || first >= p.B) break;
     base += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+    len = first + lane < p.B ? visible_keys(p, p.lens[first + lane]) : 0;
+    own = tiles_of(len);
+    incl = scan64(own);
   }
   return r;
 }
@@ -111,6 +118,15 @@ __host__ __device__ constexpr int blocks_for(int G) { return G <= 16 ? 1 : G <= 
 __host__ __device__ __forceinline__ int rows_kept(int G) { return G < 16 * blocks_for(G) ? G : 16 * blocks_for(G); }
 // floats of one wave's sums: rows of O, then (reference maximum, sum) of each row
 __host__ __device__ __forceinline__ int partial_floats(int rows, int d) { return rows * d + (2 * rows + 3) / 4 * 4; }
+// What the second kernel has to know of each (sequence, unit), behind the sums: written by the wave that takes its first tile (first, all)
+// and, where that is another one, by the wave that takes its last (last).
+struct Split {
+  int first;  // 2 * wave + which of its two sums the first part is; -1: one wave took it all
+  int last;   // the wave of the last part
+  int all;    // tiles of the whole list where there are fewer than waves (a wave then has one of them at most), else 0
+  int unused;
+};
+__host__ __device__ __forceinline__ size_t split_offset(int rows, int d) { return (size_t)2 * kWorkers * partial_floats(rows, d) * sizeof(float); }
 
 template <int D, bool FP8, int NQ>
 __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeParams p) {
@@ -125,11 +141,9 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG;
   const int page_mask = (1 << p.page_log2) - 1;
 
-  const unsigned long long all = count_tiles(p) * (unsigned)units;
-  const unsigned long long begin = (all * worker) >> kWorkersLog2, end = (all * (worker + 1)) >> kWorkersLog2;
-  if (begin == end) return;
-  int n = (int)(end - begin);  // (at most 2^59 / 2^10 tiles are ever asked for; a cache that fits the memory has far below 2^31)
-  const Place at = place_of(p, begin, units);
+  const Piece at = piece_of(p, worker, units);
+  if (at.begin == at.end) return;
+  const int n = (int)(at.end - at.begin);  // (2^10 waves share far below 2^41 tiles: a cache fits the memory)
 
   // A position in the list: tile t of `unit` of sequence b, and what its two page entries are
   struct Position {
@@ -155,12 +169,17 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   };
   Position ld;
   {
-    const unsigned long long rest = begin - at.before * (unsigned)units;
+    const unsigned long long rest = at.begin - at.before * (unsigned)units;
     ld.b = at.b;
     ld.len = at.len;
     ld.nt = tiles_of(at.len);
-    ld.unit = uniform((int)(rest / (unsigned)ld.nt));
-    ld.t = uniform((int)(rest - (unsigned long long)ld.unit * (unsigned)ld.nt));
+    if (rest >> 32 == 0) {  // (a quotient of 32 bits is a fifth of one of 64)
+      ld.unit = uniform((int)((uint32_t)rest / (uint32_t)ld.nt));
+      ld.t = uniform((int)((uint32_t)rest - (uint32_t)ld.unit * (uint32_t)ld.nt));
+    } else {
+      ld.unit = uniform((int)(rest / (unsigned)ld.nt));
+      ld.t = uniform((int)(rest - (unsigned long long)ld.unit * (unsigned)ld.nt));
+    }
   }
   Position cp = ld;
   entries(ld);
@@ -229,8 +248,18 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     }
   };
   const int kept = rows_kept(G);
-  auto finish = [&](bool whole, int part) __attribute__((always_inline)) {
+  auto finish = [&](bool head, bool tail, int part) __attribute__((always_inline)) {  // (with the first tile, with the last)
     const int hk = cp.unit / QG, first = (cp.unit - hk * QG) * 16 * NQ;
+    const bool whole = head && tail;
+    if (lane == 0 && (head || tail)) {
+      Split* const x = (Split*)((char*)p.ws + split_offset(kept, D)) + ((size_t)cp.b * units + cp.unit);
+      if (head) {
+        x->first = whole ? -1 : 2 * worker + part;
+        x->all = at.all < kWorkers ? (int)at.all : 0;
+      } else {
+        x->last = worker;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int r = 16 * i + j16;
@@ -389,8 +418,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
 
     const bool last = cp.t + 1 == cp.nt;
     if (last || i + 1 == n) {
-      const bool whole = last && began == 0;
-      finish(whole, part);
+      finish(began == 0, last, part);
       part = 1;
       if (i + 1 < n) {
         advance(cp);
@@ -404,62 +432,36 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
 }
 
 // Joins what the waves left of the (sequence, key head) pairs that more than one of them took, and writes the rows of sequences
-// without keys.  One wave per query row; WAVES of them share a row where there are few rows, each with many parts.
+// without keys.  WAVES waves for a query row: one, or, where there are few rows, each with many parts, sixteen.
 template <int D, int WAVES>
-__global__ void __launch_bounds__(256) kv_join_kernel(const DecodeParams p, int NQ) {
-  constexpr int LPR = D / 4, PER = 64 / LPR;  // lanes of a row, parts a wave adds at once
-  __shared__ float so[4][D], sm[4], sl[4];
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(const DecodeParams p, int NQ) {
+  constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, parts a wave takes side by side and requests in a row
   const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int row = WAVES == 1 ? blockIdx.x * 4 + w : blockIdx.x;
   if (row >= p.B * p.Hq) return;  // (WAVES 1: no barrier follows)
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG, kept = rows_kept(G);
   const int b = row / p.Hq, hq = row - b * p.Hq, hk = hq / G, qg = (hq - hk * G) / (16 * NQ), r = hq - hk * G - qg * 16 * NQ;
+  const int* const split = (const int*)((const char*)p.ws + split_offset(kept, D)) + ((size_t)b * units + hk * QG + qg) * 4;
   const int len = visible_keys(p, scalar_load(p.lens, b));
+  const int split_first = scalar_load(split, 0), w1 = scalar_load(split, 1), all = scalar_load(split, 2);
   const size_t out = (size_t)row * D;
-  if (len == 0) {
-    if (WAVES == 1 || w == 0) {
+  if (len == 0) {  // (nothing was written for it)
+    if (w == 0 || WAVES == 1) {
       for (int i = lane; i < D / 2; i += 64) ((uint32_t*)p.o)[out / 2 + i] = 0;
       if (lane == 0) p.lse[row] = -__builtin_inff();
     }
     return;
   }
-  // tiles in front of the sequence, and all of them
-  unsigned long long mine = 0, front = 0;
-  for (int x = lane; x < p.B; x += 64) {
-    const int nt = tiles_of(visible_keys(p, p.lens[x]));
-    mine += nt;
-    if (x < b) front += nt;
-  }
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) {
-    mine += __shfl_xor(mine, k);
-    front += __shfl_xor(front, k);
-  }
-  const unsigned long long all = uniform(mine) * (unsigned)units, nt = tiles_of(len);
-  const unsigned long long first = uniform(front) * (unsigned)units + (unsigned long long)(hk * QG + qg) * nt, last = first + nt - 1;
-  const int w0 = uniform((int)((((first + 1) << kWorkersLog2) - 1) / all)), w1 = uniform((int)((((last + 1) << kWorkersLog2) - 1) / all));
-  if (w0 == w1) return;  // one wave took it all
-  const int part0 = ((all * w0) >> kWorkersLog2) < first ? 1 : 0;
-  const int stride = partial_floats(kept, D);
-  const float* const ws = (const float*)p.ws;
+  if (split_first < 0) return;
+  // (kept inside the workspace whatever it holds: `lens` may have changed under the call)
+  const int first_sum = min(split_first, 2 * kWorkers - 1), w0 = first_sum >> 1, stride = partial_floats(kept, D);
+  // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile
+  const int parts = min(all ? tiles_of(len) : w1 - w0 + 1, kWorkers - w0);
+  const uint32_t first = all ? ((uint32_t)all * (uint32_t)w0) >> kWorkersLog2 : 0;
 
   const int sub = lane / LPR, col = (lane % LPR) * 4;
   float m = -__builtin_inff(), l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile
-  const bool sparse = all < kWorkers;
-  const int parts = sparse ? (int)nt : w1 - w0 + 1;
-  for (int i = (WAVES == 1 ? 0 : w * PER) + sub; i < parts; i += PER * WAVES) {
-    const int x = sparse ? (int)(((((uint32_t)first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all) : w0 + i;
-    const float* const src = ws + (size_t)(2 * x + (x == w0 ? part0 : 0)) * stride;
-    const f32x4 po = *(const f32x4*)(src + r * D + col);
-    const float pm = src[kept * D + 2 * r], pl = src[kept * D + 2 * r + 1];
-    const float m_new = fmaxf(m, pm), ref = m_new == -__builtin_inff() ? 0.f : m_new;
-    const float a = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2), c = __builtin_amdgcn_exp2f((pm - ref) * p.scale_log2);
-    o = o * a + po * c;
-    l = l * a + pl * c;
-    m = m_new;
-  }
   auto merge = [&](float om, float ol, const f32x4& oo) __attribute__((always_inline)) {
     const float m_new = fmaxf(m, om), ref = m_new == -__builtin_inff() ? 0.f : m_new;
     const float a = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2), c = __builtin_amdgcn_exp2f((om - ref) * p.scale_log2);
@@ -467,6 +469,22 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const DecodeParams p, int 
     l = l * a + ol * c;
     m = m_new;
   };
+  for (int i0 = (WAVES == 1 ? 0 : w * PER * AT_ONCE) + sub; i0 < parts; i0 += PER * AT_ONCE * WAVES) {
+    f32x4 po[AT_ONCE];
+    float pm[AT_ONCE], pl[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const int i = min(i0 + k * PER, parts - 1);
+      const int x = all ? (int)((((first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all) : w0 + i;
+      const float* const src = (const float*)p.ws + (size_t)(i == 0 ? first_sum : min(2 * x, 2 * kWorkers - 1)) * stride;
+      po[k] = *(const f32x4*)(src + r * D + col);
+      pm[k] = src[kept * D + 2 * r];
+      pl[k] = src[kept * D + 2 * r + 1];
+    }
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k)
+      if (i0 + k * PER < parts) merge(pm[k], pl[k], po[k]);
+  }
 #pragma unroll
   for (int k = LPR; k < 64; k *= 2) {
     const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
@@ -476,6 +494,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const DecodeParams p, int 
     merge(om, ol, oo);
   }
   if constexpr (WAVES > 1) {
+    __shared__ float so[WAVES][D], sm[WAVES], sl[WAVES];
     if (sub == 0) *(f32x4*)&so[w][col] = o;
     if (lane == 0) {
       sm[w] = m;
@@ -483,7 +502,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const DecodeParams p, int 
     }
     __syncthreads();
     if (w != 0) return;
-    for (int k = 1; k < 4; ++k) merge(sm[k], sl[k], *(const f32x4*)&so[k][col]);
+    for (int k = 1; k < min(WAVES, (parts + PER * AT_ONCE - 1) / (PER * AT_ONCE)); ++k) merge(sm[k], sl[k], *(const f32x4*)&so[k][col]);
   }
   if (sub != 0) return;
   const float inv = l == 0.f ? 0.f : p.out_scale / l;
@@ -501,8 +520,9 @@ void launch_decode(const DecodeParams& p, int nq, hipStream_t stream) {
 
 template <int D>
 void launch_join(const DecodeParams& p, int nq, hipStream_t stream) {
-  const int rows = p.B * p.Hq;
-  if (rows <= 1024) kv_join_kernel<D, 4><<<rows, 256, 0, stream>>>(p, nq);
+  const int rows = p.B * p.Hq, G = p.Hq / p.Hkv;
+  // 1024 waves leave about 1024 / (sequences x units) parts of each; one wave takes 8 (d = 64: 16) at a time
+  if ((long long)p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq)) < 64) kv_join_kernel<D, 16><<<rows, 1024, 0, stream>>>(p, nq);
   else kv_join_kernel<D, 1><<<(rows + 3) / 4, 256, 0, stream>>>(p, nq);
 }
 
@@ -521,6 +541,6 @@ int kv_decode_launch(const DecodeParams& p, int d, bool fp8, hipStream_t stream)
 }
 
 long long kv_decode_bytes(int B, int Hq, int Hkv, int d) {
-  (void)B;
-  return 2ll * kWorkers * partial_floats(rows_kept(Hq / Hkv), d) * (long long)sizeof(float);
+  const int G = Hq / Hkv, nq = blocks_for(G);
+  return (long long)split_offset(rows_kept(G), d) + (long long)B * Hkv * ((G + 16 * nq - 1) / (16 * nq)) * (long long)sizeof(Split);
 }
