@@ -3,19 +3,19 @@
 // The call reads every visible key and value once and does 4 G operations on each of their features (G query heads share a
 // key head), so it is bound by memory as long as the products run on the matrix cores and enough bytes are in flight.
 //
-// Split: the work is the list of all 32-key tiles, sequence by sequence, key head by key head; each of kWorkers waves takes an
-// equal, consecutive piece of it, whatever the lengths are.  What the pieces are follows from `lens` on the device, by a scan over them
-// that every wave does for itself.  A wave that covers all tiles of a (sequence, key head) writes its rows of o; a wave that covers
-// some of them leaves its sums (32 bits) in the workspace, at most two per wave (where its piece begins and where it ends), and the
-// second kernel joins them.
+// Split: the work is the list of all tiles (8 KB of keys: 32, 64 or 128 of them, and their values), sequence by sequence, key head by
+// key head; each of kWorkers waves takes an equal, consecutive piece of it, whatever the lengths are.  What the pieces are follows from
+// `lens` on the device, by a scan over them that every wave does for itself.  A wave that covers all tiles of a (sequence, key head) writes its
+// rows of o; a wave that covers some of them leaves its sums (32 bits) in the workspace, at most two per wave (where its piece begins and
+// where it ends), and the second kernel joins them.
 //
-// A wave streams its tiles through a ring of its own in LDS (32 KB: 128 KB of a CU's four waves, of which at least half is in flight),
-// by direct-to-LDS loads, so that no barrier is needed anywhere.  Page entries come through the scalar cache, whose counter is not the
-// tiles'.  A 16-row half of a tile lies in one page (pages hold 16 rows or more).
+// A wave streams its tiles through a ring of its own in LDS (two of 16 KB: 128 KB of a CU's four waves, of which at least half is in
+// flight), by direct-to-LDS loads, so that no barrier is needed anywhere.  Page entries come through the scalar cache, whose counter is
+// not the tiles'.  A block of 16 rows lies in one page (pages hold 16 rows or more).
 //
-// Products are taken transposed, as in attn_fwd: S^T = K Q^T and O^T += V^T P^T on the 16x16x32 MFMA, the queries of the
-// group as its 16 columns (NQ blocks of them, fed by the same keys).  A lane then holds keys 4 g + r of both halves of a tile for one query, which
-// are the eight k of its second operand in place: key 4 g + r of half e is k = 8 g + 4 e + r, and V is read (transposing LDS loads)
+// Products are taken transposed, as in attn_fwd: S^T = K Q^T and O^T += V^T P^T on the 16x16x32 MFMA, the queries of the group as its
+// 16 columns (NQ blocks of them, fed by the same keys).  A lane then holds keys 4 g + r of both blocks of 32 keys for one query, which
+// are the eight k of its second operand in place: key 4 g + r of block e is k = 8 g + 4 e + r, and V is read (transposing LDS loads)
 // in the same order.
 #include <type_traits>
 
@@ -39,7 +39,15 @@ __device__ __forceinline__ unsigned long long uniform(unsigned long long x) {
 __device__ __forceinline__ int scalar_load(const int* p, size_t i) { return ((const __attribute__((address_space(4))) int*)p)[i]; }
 
 __device__ __forceinline__ int visible_keys(const DecodeParams& p, int len) { return min(max(len, 0), p.W << p.page_log2); }
-__device__ __forceinline__ int tiles_of(int keys) { return (keys + 31) >> 5; }
+
+// A tile is 8 KB of keys: 32 rows of 256 bytes, 64 of 128, 128 of 64.  (Tiles of 32 keys throughout cost the same time per tile, about 3000
+// cycles of one wave, for a half or a quarter of the bytes: 66 us for 32 ragged e4m3 sequences up to 9000 where the memory needs 57.)
+template <int ROWB>
+constexpr int kTileLog2 = ROWB == 256 ? 5 : ROWB == 128 ? 6 : 7;
+template <int TL>
+__device__ __forceinline__ int tiles_of(int keys) {
+  return (keys + (1 << TL) - 1) >> TL;
+}
 
 // inclusive sums over the lanes: shifts inside rows of 16, then the rows' last sums
 __device__ __forceinline__ uint32_t scan64(uint32_t x) {
@@ -58,16 +66,17 @@ struct Piece {
   int b, len;                 // the sequence and its visible keys
   unsigned long long before;  // tiles of one key head in front of it
 };
+template <int TL>
 __device__ __forceinline__ Piece piece_of(const DecodeParams& p, int worker, int units) {
   const int lane = threadIdx.x & 63;
   Piece r;
-  // (a sequence has at most 2^25 tiles: sums over 64 of them fit 32 bits)
+  // (a sequence has at most 2^25 tiles of 32 keys: sums over 64 of them fit 32 bits)
   int len = lane < p.B ? visible_keys(p, p.lens[lane]) : 0;
-  uint32_t own = tiles_of(len), incl = scan64(own);
+  uint32_t own = tiles_of<TL>(len), incl = scan64(own);
   unsigned long long total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
   if (p.B > 64) {
     unsigned long long mine = 0;
-    for (int b = 64 + lane; b < p.B; b += 64) mine += tiles_of(visible_keys(p, p.lens[b]));
+    for (int b = 64 + lane; b < p.B; b += 64) mine += tiles_of<TL>(visible_keys(p, p.lens[b]));
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) mine += __shfl_xor(mine, m);
     total += uniform(mine);
@@ -89,7 +98,7 @@ __device__ __forceinline__ Piece piece_of(const DecodeParams& p, int worker, int
     if (n < 64 || first >= p.B) break;
     base += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
     len = first + lane < p.B ? visible_keys(p, p.lens[first + lane]) : 0;
-    own = tiles_of(len);
+    own = tiles_of<TL>(len);
     incl = scan64(own);
   }
   return r;
@@ -130,10 +139,12 @@ __host__ __device__ __forceinline__ size_t split_offset(int rows, int d) { retur
 
 template <int D, bool FP8, int NQ>
 __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeParams p) {
-  constexpr int ROWB = D * (FP8 ? 1 : 2), NCH = ROWB / 16, TILEB = 32 * ROWB;
+  constexpr int ROWB = D * (FP8 ? 1 : 2), NCH = ROWB / 16, TL = kTileLog2<ROWB>, KT = 1 << TL, TILEB = KT * ROWB;
+  constexpr int NB = KT / 16, NP = KT / 32;                    // blocks of 16 keys, pairs of them
   constexpr int LPT = TILEB / 1024, PIECE_ROWS = 1024 / ROWB;  // direct loads of a tile of keys or values, rows of one
-  constexpr int RING = 32768 / (2 * TILEB), NDB = D / 16, NKS = D / 32;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * 32768];
+  constexpr int LPB = LPT / NB > 0 ? LPT / NB : 1, RING = 2, NDB = D / 16, NKS = D / 32;
+  static_assert(TILEB == 8192 && PIECE_ROWS <= 16 && LPB * NB == LPT, "a direct load stays inside a block of 16 keys");
+  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * RING * 2 * TILEB];
   LDS_AS char* const smem = (LDS_AS char*)smem_raw;
 
   const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, j16 = lane & 15, g = lane >> 4;
@@ -141,19 +152,21 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG;
   const int page_mask = (1 << p.page_log2) - 1;
 
-  const Piece at = piece_of(p, worker, units);
+  const Piece at = piece_of<TL>(p, worker, units);
   if (at.begin == at.end) return;
   const int n = (int)(at.end - at.begin);  // (2^10 waves share far below 2^41 tiles: a cache fits the memory)
 
-  // A position in the list: tile t of `unit` of sequence b, and what its two page entries are
+  // A position in the list: tile t of `unit` of sequence b, and the page entries of its blocks
   struct Position {
-    int b, unit, t, nt, len, e0, e1;
+    int b, unit, t, nt, len, e[NB];
   };
   auto entries = [&](Position& x) __attribute__((always_inline)) {
-    const int j = x.t << 5;
     const size_t row = (size_t)x.b * p.W;
-    x.e0 = scalar_load(p.pages, row + (j >> p.page_log2));
-    x.e1 = j + 16 < x.len ? scalar_load(p.pages, row + ((j + 16) >> p.page_log2)) : -1;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int j = (x.t << TL) + 16 * i;  // (below len in block 0: there is no tile without keys)
+      x.e[i] = scalar_load(p.pages, row + ((i == 0 || j < x.len ? j : x.t << TL) >> p.page_log2));
+    }
   };
   auto advance = [&](Position& x) __attribute__((always_inline)) {
     if (++x.t < x.nt) return;
@@ -165,14 +178,14 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       ++x.b;
       x.len = visible_keys(p, scalar_load(p.lens, x.b));
     } while (x.len == 0);
-    x.nt = tiles_of(x.len);
+    x.nt = tiles_of<TL>(x.len);
   };
   Position ld;
   {
     const unsigned long long rest = at.begin - at.before * (unsigned)units;
     ld.b = at.b;
     ld.len = at.len;
-    ld.nt = tiles_of(at.len);
+    ld.nt = tiles_of<TL>(at.len);
     if (rest >> 32 == 0) {  // (a quotient of 32 bits is a fifth of one of 64)
       ld.unit = uniform((int)((uint32_t)rest / (uint32_t)ld.nt));
       ld.t = uniform((int)((uint32_t)rest - (uint32_t)ld.unit * (uint32_t)ld.nt));
@@ -184,46 +197,51 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   Position cp = ld;
   entries(ld);
 
-  // ---- direct loads: piece c of a half tile is rows c * PIECE_ROWS + lane / NCH; chunks are swizzled on the global side ----
-  uint32_t koff[LPT / 2], voff[LPT / 2];
+  // ---- direct loads: piece c of a block is rows c * PIECE_ROWS + lane / NCH; chunks are swizzled on the global side (the swizzles
+  // repeat every 16 rows) ----
+  uint32_t koff[LPB], voff[LPB];
 #pragma unroll
-  for (int c = 0; c < LPT / 2; ++c) {
+  for (int c = 0; c < LPB; ++c) {
     const int r = c * PIECE_ROWS + lane / NCH, ch = lane % NCH;
     koff[c] = r * ROWB + ((ch ^ attn_swz_k<ROWB>(r)) << 4);
     voff[c] = r * ROWB + ((ch ^ (FP8 ? attn_swz_k<ROWB>(r) : attn_swz_v<ROWB>(r))) << 4);
   }
-  const uint32_t ring = (uint32_t)(uintptr_t)smem + w * 32768;
-  // requests tile `ld` into `slot`; the result tells which of its halves have a page.  What has none is read from where the other half
-  // lies (or the cache's first rows) and hidden later.
+  const uint32_t wave_base = w * (RING * 2 * TILEB), ring = (uint32_t)(uintptr_t)smem + wave_base;
+  // Requests tile `ld` into `slot`; bit i of the result: block i has a page and a key.  A block that has none is read from where the tile
+  // begins (or the cache's first rows) and hidden later.
   auto issue = [&](int slot) __attribute__((always_inline)) {
-    const int j = ld.t << 5, hk = ld.unit / QG;
-    const bool ok0 = (unsigned)ld.e0 < (unsigned)p.num_pages, ok1 = (unsigned)ld.e1 < (unsigned)p.num_pages;
-    const size_t a0 = ok0 ? ((((size_t)ld.e0 * p.Hkv + hk) << p.page_log2) + (j & page_mask)) * ROWB : 0;
-    const size_t a1 = ok1 ? ((((size_t)ld.e1 * p.Hkv + hk) << p.page_log2) + ((j + 16) & page_mask)) * ROWB : a0;
-    const char* const k = (const char*)p.k;
-    const char* const v = (const char*)p.v;
+    const int j0 = ld.t << TL, hk = ld.unit / QG;
+    size_t from[NB];
+    uint32_t ok = 0;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const bool has = (unsigned)ld.e[i] < (unsigned)p.num_pages;
+      from[i] = has ? ((((size_t)ld.e[i] * p.Hkv + hk) << p.page_log2) + ((j0 + (j0 + 16 * i < ld.len ? 16 * i : 0)) & page_mask)) * ROWB : 0;
+      ok |= has && j0 + 16 * i < ld.len ? 1u << i : 0u;
+    }
     const uint32_t to = ring + slot * (2 * TILEB);
 #pragma unroll
-    for (int c = 0; c < LPT; ++c) attn_lds_dma16(k + (c < LPT / 2 ? a0 : a1), koff[c % (LPT / 2)], to + c * 1024);
+    for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.k + from[c / LPB], koff[c % LPB], to + c * 1024);
 #pragma unroll
-    for (int c = 0; c < LPT; ++c) attn_lds_dma16(v + (c < LPT / 2 ? a0 : a1), voff[c % (LPT / 2)], to + TILEB + c * 1024);
-    return (ok0 ? 1u : 0u) | (ok1 ? 2u : 0u);
+    for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.v + from[c / LPB], voff[c % LPB], to + TILEB + c * 1024);
+    return ok;
   };
 
-  // ---- operand addresses in slot 0 ----
-  uint32_t ka[FP8 ? D / 64 : NKS], va[NDB][2];
+  // ---- operand addresses in slot 0, first block or pair ----
+  constexpr int NKR = FP8 ? D / 64 : NKS;  // 16-byte reads of a key row: e4m3 rows hold two k-steps in one
+  uint32_t ka[NKR], va[NDB][2];
 #pragma unroll
-  for (int s = 0; s < (FP8 ? D / 64 : NKS); ++s) ka[s] = w * 32768 + j16 * ROWB + (((4 * s + g) ^ attn_swz_k<ROWB>(j16)) << 4);
+  for (int s = 0; s < NKR; ++s) ka[s] = wave_base + j16 * ROWB + (((4 * s + g) ^ attn_swz_k<ROWB>(j16)) << 4);
 #pragma unroll
   for (int db = 0; db < NDB; ++db)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      if constexpr (FP8) {  // eight rows of one column: 4 g .. 4 g + 3 of both halves
+      if constexpr (FP8) {  // eight rows of one column: 4 g .. 4 g + 3 of both blocks
         const int i = j16 >> 1, r = (i < 4 ? 0 : 16) + 4 * g + (i & 3);
-        va[db][e] = w * 32768 + TILEB + r * ROWB + ((db ^ attn_swz_k<ROWB>(r)) << 4) + ((j16 & 1) << 3);
-      } else {  // four rows, 4 g .. 4 g + 3 of half e
+        va[db][e] = wave_base + TILEB + r * ROWB + ((db ^ attn_swz_k<ROWB>(r)) << 4) + ((j16 & 1) << 3);
+      } else {  // four rows, 4 g .. 4 g + 3 of block e
         const int r = 16 * e + 4 * g + (j16 >> 2);
-        va[db][e] = w * 32768 + TILEB + r * ROWB + (((2 * db + ((j16 & 3) >> 1)) ^ attn_swz_v<ROWB>(r)) << 4) + ((j16 & 1) << 3);
+        va[db][e] = wave_base + TILEB + r * ROWB + (((2 * db + ((j16 & 3) >> 1)) ^ attn_swz_v<ROWB>(r)) << 4) + ((j16 & 1) << 3);
       }
     }
 
@@ -238,7 +256,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       const char* const src = (const char*)p.q + ((size_t)cp.b * p.Hq + (size_t)hk * G + h) * (D * 2);
 #pragma unroll
       for (int s = 0; s < NKS; ++s) {
-        const int f = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;  // (e4m3: a 16-byte read holds two steps)
+        const int f = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
         q[i][s] = __builtin_bit_cast(bf16x8, h < G ? *(const u32x4*)(src + f * 2) : u32x4{0, 0, 0, 0});
       }
 #pragma unroll
@@ -284,57 +302,48 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       }
     }
   };
+  // waits until at most N loads of this tile are under way (and those of the tile behind it, where one is requested)
+  auto wait = [&](auto value, bool behind) __attribute__((always_inline)) {
+    constexpr int N = decltype(value)::value;
+    if (behind) ATTN_WAIT_VMCNT(2 * LPT + N);
+    else ATTN_WAIT_VMCNT(N);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
 
-  uint32_t have = 0;  // two bits for each tile in the ring: which halves have a page
-  const int ahead = min(n, RING);
+  uint32_t have = 0;  // NB bits for each tile in the ring
   start();
-  int began = cp.t;
-  for (int i = 0; i < ahead; ++i) {
-    have |= issue(i) << (2 * i);
+  int began = cp.t, slot = 0, part = 0;
+  for (int i = 0; i < min(n, RING); ++i) {
+    have |= issue(i) << (NB * i);
     if (i + 1 < n) {
       advance(ld);
       entries(ld);
     }
   }
-  int slot = 0, part = 0;
   for (int i = 0; i < n; ++i) {
-    const int base = slot * (2 * TILEB), left = min(n - 1 - i, RING - 1);  // tiles requested behind this one
-    auto wait = [&](auto value) __attribute__((always_inline)) {
-      constexpr int V = decltype(value)::value;  // loads of this tile that may still be under way
-      switch (left) {
-        case 0: ATTN_WAIT_VMCNT(V); break;
-        case 1: ATTN_WAIT_VMCNT(2 * LPT * (RING > 1 ? 1 : 0) + V); break;
-        case 2: ATTN_WAIT_VMCNT(2 * LPT * (RING > 2 ? 2 : 0) + V); break;
-        case 3: ATTN_WAIT_VMCNT(2 * LPT * (RING > 3 ? 3 : 0) + V); break;
-        case 4: ATTN_WAIT_VMCNT(2 * LPT * (RING > 4 ? 4 : 0) + V); break;
-        case 5: ATTN_WAIT_VMCNT(2 * LPT * (RING > 5 ? 5 : 0) + V); break;
-        case 6: ATTN_WAIT_VMCNT(2 * LPT * (RING > 6 ? 6 : 0) + V); break;
-        default: ATTN_WAIT_VMCNT(2 * LPT * (RING > 7 ? 7 : 0) + V); break;
-      }
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    wait(std::integral_constant<int, LPT>{});
+    const int base = slot * (2 * TILEB);
+    const bool behind = i + 1 < n;
+    wait(std::integral_constant<int, LPT>{}, behind);
 
-    // visible rows of the tile's halves
-    const int keys = cp.len - (cp.t << 5);
-    const int n0 = have & 1 ? min(keys, 16) : 0, n1 = have & 2 ? min(max(keys - 16, 0), 16) : 0;
-    const bool hidden = n0 + n1 < 32;
+    // visible rows of the tile's blocks
+    const int keys = cp.len - (cp.t << TL);
+    auto rows = [&](int e) __attribute__((always_inline)) { return have >> e & 1 ? min(keys - 16 * e, 16) : 0; };
+    const bool hidden = keys < KT || (have & ((1u << NB) - 1)) != (1u << NB) - 1;
 
-    f32x4 s[NQ][2];
+    f32x4 s[NQ][NB];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < NB; ++e) {
       bf16x8 k[NKS];
-      if constexpr (FP8) {
 #pragma unroll
-        for (int x = 0; x < D / 64; ++x) {
-          const u32x4 c = *(LDS_AS u32x4*)(smem + ka[x] + base + e * 16 * ROWB);
+      for (int x = 0; x < NKR; ++x) {
+        const u32x4 c = *(LDS_AS u32x4*)(smem + ka[x] + base + e * 16 * ROWB);
+        if constexpr (FP8) {
           k[2 * x] = e4m3_to_bf16(c[0], c[1]);
           k[2 * x + 1] = e4m3_to_bf16(c[2], c[3]);
+        } else {
+          k[x] = __builtin_bit_cast(bf16x8, c);
         }
-      } else {
-#pragma unroll
-        for (int x = 0; x < NKS; ++x) k[x] = __builtin_bit_cast(bf16x8, *(LDS_AS u32x4*)(smem + ka[x] + base + e * 16 * ROWB));
       }
 #pragma unroll
       for (int i2 = 0; i2 < NQ; ++i2) {
@@ -345,76 +354,83 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     }
     if (hidden) {
 #pragma unroll
-      for (int i2 = 0; i2 < NQ; ++i2)
+      for (int e = 0; e < NB; ++e)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int i2 = 0; i2 < NQ; ++i2)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (4 * g + r >= (e ? n1 : n0)) s[i2][e][r] = -__builtin_inff();
+            if (4 * g + r >= rows(e)) s[i2][e][r] = -__builtin_inff();
     }
 
     // streaming softmax; differences are taken before they are scaled, so that scores near the type's lowest value do not overflow
-    bf16x8 pr[NQ];
+    bf16x8 pr[NQ][NP];
 #pragma unroll
     for (int i2 = 0; i2 < NQ; ++i2) {
       float mx = s[i2][0][0];
 #pragma unroll
-      for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[i2][x >> 2][x & 3]);
+      for (int x = 1; x < 4 * NB; ++x) mx = fmaxf(mx, s[i2][x >> 2][x & 3]);
       const float m_new = fmaxf(m[i2], max_rows(mx)), ref = m_new == -__builtin_inff() ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f((m[i2] - ref) * p.scale_log2);
       if (__any(m_new != m[i2])) {
+        const float alpha = __builtin_amdgcn_exp2f((m[i2] - ref) * p.scale_log2);
 #pragma unroll
         for (int db = 0; db < NDB; ++db) o[i2][db] *= alpha;
         l[i2] *= alpha;
       }
       m[i2] = m_new;
-      float e[8], sum = 0.f;
+      float sum = 0.f;
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        e[x] = __builtin_amdgcn_exp2f((s[i2][x >> 2][x & 3] - ref) * p.scale_log2);
-        sum += e[x];
+      for (int x = 0; x < NP; ++x) {
+        float e[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          e[y] = __builtin_amdgcn_exp2f((s[i2][2 * x + (y >> 2)][y & 3] - ref) * p.scale_log2);
+          sum += e[y];
+        }
+        // bf16 for the matrix cores: half a step of each probability, as in attn_fwd
+        pr[i2][x] = __builtin_bit_cast(bf16x8, u32x4{attn_pack_bf16(e[0], e[1]), attn_pack_bf16(e[2], e[3]), attn_pack_bf16(e[4], e[5]), attn_pack_bf16(e[6], e[7])});
       }
       l[i2] += sum;  // (of the unrounded probabilities, this lane's keys)
-      // bf16 for the matrix cores: half a step of each probability, as in attn_fwd
-      pr[i2] = __builtin_bit_cast(bf16x8, u32x4{attn_pack_bf16(e[0], e[1]), attn_pack_bf16(e[2], e[3]), attn_pack_bf16(e[4], e[5]), attn_pack_bf16(e[6], e[7])});
     }
 
-    wait(std::integral_constant<int, 0>{});
+    wait(std::integral_constant<int, 0>{}, behind);
     if (hidden) {  // 0 times what lies in a hidden row would be NaN where that is not finite
 #pragma unroll
       for (int c = 0; c < LPT; ++c) {
-        const int r = (c % (LPT / 2)) * PIECE_ROWS + lane / NCH;
-        if (r >= (c < LPT / 2 ? n0 : n1)) *(LDS_AS u32x4*)(smem + w * 32768 + base + TILEB + c * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        const int r = (c % LPB) * PIECE_ROWS + lane / NCH;
+        if (r >= rows(c / LPB)) *(LDS_AS u32x4*)(smem + wave_base + base + TILEB + c * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      bf16x8 v;
-      if constexpr (FP8) {
-        const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)(smem + va[db][0] + base));
-        v = e4m3_to_bf16((uint32_t)c[0], (uint32_t)c[1]);
-      } else {
-        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(smem + va[db][0] + base));
-        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(smem + va[db][1] + base));
-        v = __builtin_bit_cast(bf16x8, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
-      }
+    for (int x = 0; x < NP; ++x)
 #pragma unroll
-      for (int i2 = 0; i2 < NQ; ++i2) o[i2][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[i2], o[i2][db], 0, 0, 0);
-    }
+      for (int db = 0; db < NDB; ++db) {
+        bf16x8 v;
+        const int at_pair = base + x * 32 * ROWB;
+        if constexpr (FP8) {
+          const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)(smem + va[db][0] + at_pair));
+          v = e4m3_to_bf16((uint32_t)c[0], (uint32_t)c[1]);
+        } else {
+          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(smem + va[db][0] + at_pair));
+          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(smem + va[db][1] + at_pair));
+          v = __builtin_bit_cast(bf16x8, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
+        }
+#pragma unroll
+        for (int i2 = 0; i2 < NQ; ++i2) o[i2][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[i2][x], o[i2][db], 0, 0, 0);
+      }
 
     // the slot is free once its last operand has arrived
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    have >>= 2;
+    have >>= NB;
     if (i + RING < n) {
-      have |= issue(slot) << (2 * (RING - 1));
+      have |= issue(slot) << (NB * (RING - 1));
       if (i + RING + 1 < n) {
         advance(ld);
         entries(ld);
       }
     }
-    slot = slot == RING - 1 ? 0 : slot + 1;
+    slot ^= 1;
 
     const bool last = cp.t + 1 == cp.nt;
     if (last || i + 1 == n) {
@@ -434,7 +450,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
 // Joins what the waves left of the (sequence, key head) pairs that more than one of them took, and writes the rows of sequences
 // without keys.  WAVES waves for a query row: one, or, where there are few rows, each with many parts, sixteen.
 template <int D, int WAVES>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(const DecodeParams p, int NQ) {
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(const DecodeParams p, int NQ, int tile_log2) {
   constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, parts a wave takes side by side and requests in a row
   const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int row = WAVES == 1 ? blockIdx.x * 4 + w : blockIdx.x;
@@ -456,7 +472,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(
   // (kept inside the workspace whatever it holds: `lens` may have changed under the call)
   const int first_sum = min(split_first, 2 * kWorkers - 1), w0 = first_sum >> 1, stride = partial_floats(kept, D);
   // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile
-  const int parts = min(all ? tiles_of(len) : w1 - w0 + 1, kWorkers - w0);
+  const int parts = min(all ? (len + (1 << tile_log2) - 1) >> tile_log2 : w1 - w0 + 1, kWorkers - w0);
   const uint32_t first = all ? ((uint32_t)all * (uint32_t)w0) >> kWorkersLog2 : 0;
 
   const int sub = lane / LPR, col = (lane % LPR) * 4;
@@ -519,11 +535,11 @@ void launch_decode(const DecodeParams& p, int nq, hipStream_t stream) {
 }
 
 template <int D>
-void launch_join(const DecodeParams& p, int nq, hipStream_t stream) {
+void launch_join(const DecodeParams& p, int nq, int tile_log2, hipStream_t stream) {
   const int rows = p.B * p.Hq, G = p.Hq / p.Hkv;
   // 1024 waves leave about 1024 / (sequences x units) parts of each; one wave takes 8 (d = 64: 16) at a time
-  if ((long long)p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq)) < 64) kv_join_kernel<D, 16><<<rows, 1024, 0, stream>>>(p, nq);
-  else kv_join_kernel<D, 1><<<(rows + 3) / 4, 256, 0, stream>>>(p, nq);
+  if ((long long)p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq)) < 64) kv_join_kernel<D, 16><<<rows, 1024, 0, stream>>>(p, nq, tile_log2);
+  else kv_join_kernel<D, 1><<<(rows + 3) / 4, 256, 0, stream>>>(p, nq, tile_log2);
 }
 
 }  // namespace
@@ -535,8 +551,9 @@ int kv_decode_launch(const DecodeParams& p, int d, bool fp8, hipStream_t stream)
   else if (fp8) launch_decode<64, true>(p, nq, stream);
   else launch_decode<64, false>(p, nq, stream);
   if (hipGetLastError() != hipSuccess) return 1;
-  if (d == 128) launch_join<128>(p, nq, stream);
-  else launch_join<64>(p, nq, stream);
+  const int tile_log2 = d == 128 && !fp8 ? kTileLog2<256> : d == 64 && fp8 ? kTileLog2<64> : kTileLog2<128>;
+  if (d == 128) launch_join<128>(p, nq, tile_log2, stream);
+  else launch_join<64>(p, nq, tile_log2, stream);
   return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
