@@ -12,6 +12,7 @@ SOURCES = ["attn_api.hip", "attn_fwd_sp.hip", "attn_fwd_fp8.hip", "attn_bwd_bf16
 # what stands around attention in a layer (include/kv.h) is a library of its own: who only attends does not load it
 LIB_KV = os.path.join(HERE, "libkv_mi355x.so")
 SOURCES_KV = ["kv_api.hip", "rope.hip", "kv_decode.hip"]
+CALL_KV = os.path.join(HERE, "_kv_call.so")  # its Python side: host code, by the host compiler
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 VALU forms are switched off on purpose (they have misbehaved on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -33,11 +34,22 @@ def build(verbose: bool = True, extra_flags=()) -> str:
             print(" ".join(cmd), flush=True)
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs[src] = obj
+    import sysconfig
+
+    import torch
+
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-w",
+           "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_path("include"),
+           "-c", os.path.join(CSRC, "kv_call.cpp"), "-o", os.path.join(CSRC, "kv_call.o")]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, pr in procs:
         out, _ = pr.communicate()
         out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
         if pr.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + out)
+            raise RuntimeError("the compiler failed:\n" + " ".join(cmd) + "\n" + out)
         if verbose and out.strip():
             print(out)
     for lib, sources in ((LIB, SOURCES), (LIB_KV, SOURCES_KV)):
@@ -45,6 +57,11 @@ def build(verbose: bool = True, extra_flags=()) -> str:
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
+    tlib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-shared", os.path.join(CSRC, "kv_call.o"), "-o", CALL_KV, f"-L{HERE}", "-lkv_mi355x", f"-L{tlib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
     return LIB
 
 

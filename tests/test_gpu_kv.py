@@ -496,6 +496,15 @@ def test_kv_decode_on_two_streams_at_once():
         assert torch.equal(o, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
 
 
+def test_tensors_of_another_device_are_refused():
+    """With one GPU: the same call, told that another device is the current one."""
+    import importlib
+
+    call, t = importlib.import_module("paper_2605_10905_amd.kv")._call, torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="q is on device 0, the current one is 1"):
+        call.kv_decode(1, 0, t, *[4096] * 7, 1, 1, 1, 64, 1, 16, 1, 1.0, 0, 1.0, 1.0)
+
+
 # ---- together ----------------------------------------------------------------------------------
 
 

@@ -110,9 +110,11 @@ def test_workspace_sizes(A):
 def test_tensors_that_the_gpu_could_not_read_are_refused(A):
     """Other types, CPU tensors, strides and too few elements are errors of the binding, before the library is called."""
     bf, i32 = torch.zeros(4096, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.int32)
-    for kw, text in ((dict(q=bf.float()), "q is torch.float32"), (dict(q=bf), "q is not on a GPU"), (dict(lens=i32.long()), "lens is torch.int64"),
-                     (dict(lens=i32), "not on a GPU"), (dict(k_cache=bf, dtype=1), "k_cache is torch.bfloat16"), (dict(workspace=bf), "not torch.float32"),
-                     (dict(v_cache=bf.view(torch.uint8)), "v_cache is torch.uint8")):
+    f32 = torch.zeros(A.kv_decode_workspace_bytes(2, 4, 2, 64) // 4)
+    for kw, text in ((dict(q=bf.float()), "q is Float, not BFloat16"), (dict(q=bf), "q is not on a GPU"), (dict(lens=i32.long()), "lens is Long, not Int"),
+                     (dict(lens=i32), "not on a GPU"), (dict(k_cache=bf, dtype=1), "k_cache is BFloat16, not Byte"), (dict(workspace=bf), "not Float"),
+                     (dict(v_cache=bf.view(torch.uint8)), "v_cache is Byte, not BFloat16"), (dict(workspace=f32), "workspace is not on a GPU"),
+                     (dict(workspace=f32[1:]), "elements"), (dict(pages=i32[:3]), "pages has 3 elements, 4 are needed"), (dict(o=bf.view(64, 64).t()), "o must be contiguous")):
         with pytest.raises(ValueError, match=text):
             _decode(A, **kw)
     for call, kw in ((_rope, dict(qkv=bf)), (_rope, dict(pos=i32.float())), (_bwd, dict(dqkv=bf)), (_append, dict(seq=i32)), (_append, dict(v_cache=i32))):
@@ -120,41 +122,37 @@ def test_tensors_that_the_gpu_could_not_read_are_refused(A):
             call(A, **kw)
 
 
-class _Fake:
-    """What the binding asks of a tensor on device 0."""
-
-    def __init__(self, t, device=0):
-        self.t, self.dtype, self.shape, self.device = t, t.dtype, t.shape, device
-
-    def __getattr__(self, name):
-        return getattr(self.t, name)
-
-    def get_device(self):
-        return self.device
-
-
-def test_layouts_are_checked():
-    kv = importlib.import_module("paper_2605_10905_amd.kv")
-    bf = torch.bfloat16
-    x = torch.zeros(6, 40, dtype=bf)
-    assert kv._ptr(_Fake(x), bf, 240, 0, "x") == x.data_ptr() and kv._ptr(None, bf, 1, 0, "x") is None and kv._ptr(64, bf, 1, 0, "x") == 64
-    with pytest.raises(ValueError, match="240 elements, 241"):
-        kv._ptr(_Fake(x), bf, 241, 0, "x")
-    with pytest.raises(ValueError, match="contiguous"):
-        kv._ptr(_Fake(x.t()), bf, 1, 0, "x")
-    with pytest.raises(ValueError, match="device 1, the current one is 0"):
-        kv._ptr(_Fake(x, 1), bf, 1, 0, "x")
-    with pytest.raises(ValueError, match="device 1, the current one is 0"):
-        kv._rows(_Fake(x, 1), 40, 6, 40, 0, "x")
-    with pytest.raises(TypeError, match="list"):
-        kv._ptr([1.0], bf, 1, 0, "x")
-    for t, ld, rows, width in ((x, 40, 6, 40), (x[:, :32], 40, 6, 32), (x.view(2, 3, 40)[:, :, 8:], 40, 6, 32), (x.view(-1), 40, 6, 40), (x[:2, :32], 40, 1, 32),
-                               (x[1:5, :32], 40, 4, 24)):
-        assert kv._rows(_Fake(t), ld, rows, width, 0, "x") == t.data_ptr()
-    for t, ld, rows, width in ((x, 48, 6, 40), (x, 40, 7, 40), (x[:, :32], 40, 6, 40), (x[::2, :32], 40, 3, 32), (x[:, ::2], 40, 6, 20), (x.t(), 6, 40, 6),
-                               (x.view(2, 3, 40)[:, :2], 40, 4, 40), (x[:, :32], 32, 6, 32)):
+def test_rows_of_a_wider_buffer_are_checked(A):
+    """Views whose rows are `ld` apart are taken (the next check, of the device, is the one that fails here), others are not."""
+    x = torch.zeros(9, 320, dtype=torch.bfloat16)
+    for t, ld, B, N in ((x[:8, :256], 320, 1, 8), (x[:, 64:], 320, 1, 9), (x.view(3, 3, 320)[:, :, 8:264], 320, 3, 3), (x.view(-1), 320, 3, 3), (x, 256, 1, 8), (x[:1, :256], 320, 1, 1),
+                        (x[1:2], 320, 1, 1), (x[4:, :300], 320, 5, 1)):
+        with pytest.raises(ValueError, match="qkv is not on a GPU"):
+            _rope(A, qkv=t, ld=ld, B=B, N=N, npos=99)
+        with pytest.raises(ValueError, match="dqkv is not on a GPU"):
+            _bwd(A, dqkv=t, dld=ld, B=B, N=N, npos=99)
+    for t, ld, B, N in ((x, 336, 1, 9), (x, 320, 2, 5), (x[:, :200], 320, 1, 9), (x[::2, :256], 320, 1, 5), (x[:, :256], 256, 1, 9), (x[:, ::1].t(), 8, 1, 320),
+                        (x.view(3, 3, 320)[:, :2], 320, 3, 2), (x.view(3, 3, 320)[::2], 320, 2, 3), (x[:1, :256], 320, 1, 2), (x[:, ::5], 320, 1, 9)):
         with pytest.raises(ValueError, match="does not hold"):
-            kv._rows(_Fake(t), ld, rows, width, 0, "x")
+            _rope(A, qkv=t, ld=ld, B=B, N=N, npos=999)
+
+
+def test_arguments_that_are_no_numbers_or_tensors(A):
+    import numpy as np
+
+    with pytest.raises(TypeError):
+        _decode(A, q=[1.0])
+    with pytest.raises(TypeError):
+        _decode(A, B="2")
+    with pytest.raises(TypeError):
+        _decode(A, scale=None)
+    with pytest.raises(OverflowError):
+        _decode(A, W=2 ** 31)
+    with pytest.raises(OverflowError):
+        _rope(A, ld=2 ** 63)
+    assert _decode(A, B=np.int64(0)) == 2 and _decode(A, scale=np.float32(-1)) == 4 and _rope(A, interleaved=True, N=0) == 2
+    with pytest.raises(TypeError):
+        importlib.import_module("paper_2605_10905_amd.kv")._call.kv_decode(0, 0, 1, 2)
 
 
 _MAIN = """
