@@ -21,7 +21,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # the one-wave-per-SIMD backward kernel keeps its score accumulators in ordinary registers, where the vector work reads them.
 # (An internal switch of the compiler: known to the clang 22 of ROCm 7.2.0, with which all figures were taken.  A compiler that does not know
 # it refuses the build; without it the kernels' register plan does not hold, and the listing has to be read anew for the wait states.)
-SOURCE_FLAGS = {"attn_bwd_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# kv_decode.hip, one wave per SIMD too: its products in ordinary registers save 90 register moves a tile (16 x 2000 keys 25.7 -> 25.3 us,
+# 1 x 500 4.8 -> 4.4); nothing there depends on it.
+SOURCE_FLAGS = {"attn_bwd_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "kv_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def build(verbose: bool = True, extra_flags=()) -> str:

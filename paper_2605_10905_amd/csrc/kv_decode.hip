@@ -68,15 +68,25 @@ struct Piece {
 };
 template <int TL>
 __device__ __forceinline__ Piece piece_of(const DecodeParams& p, int worker, int units) {
+  constexpr int HELD = 4;  // lengths that a lane holds: batches of 256 are read once, longer ones twice
   const int lane = threadIdx.x & 63;
   Piece r;
   // (a sequence has at most 2^25 tiles of 32 keys: sums over 64 of them fit 32 bits)
-  int len = lane < p.B ? visible_keys(p, p.lens[lane]) : 0;
-  uint32_t own = tiles_of<TL>(len), incl = scan64(own);
-  unsigned long long total = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
-  if (p.B > 64) {
+  int len[HELD];
+  uint32_t incl[HELD];
+  unsigned long long total = 0;
+#pragma unroll
+  for (int c = 0; c < HELD; ++c) len[c] = 64 * c + lane < p.B ? p.lens[64 * c + lane] : 0;
+#pragma unroll
+  for (int c = 0; c < HELD; ++c) {
+    len[c] = visible_keys(p, len[c]);
+    incl[c] = 0;
+    if (c == 0 || p.B > 64 * c) incl[c] = scan64(tiles_of<TL>(len[c]));
+    total += (uint32_t)__builtin_amdgcn_readlane((int)incl[c], 63);
+  }
+  if (p.B > 64 * HELD) {
     unsigned long long mine = 0;
-    for (int b = 64 + lane; b < p.B; b += 64) mine += tiles_of<TL>(visible_keys(p, p.lens[b]));
+    for (int b = 64 * HELD + lane; b < p.B; b += 64) mine += tiles_of<TL>(visible_keys(p, p.lens[b]));
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) mine += __shfl_xor(mine, m);
     total += uniform(mine);
@@ -87,19 +97,25 @@ __device__ __forceinline__ Piece piece_of(const DecodeParams& p, int worker, int
   r.b = r.len = 0;
   r.before = 0;
   unsigned long long base = 0;
-  for (int first = 0;;) {
-    const uint32_t excl = incl - own;
+  // whether the sequence that the piece begins in is behind these 64; if not, it is the last of them that does not begin behind it
+  auto behind = [&](int first, int len64, uint32_t incl64) __attribute__((always_inline)) {
+    const uint32_t excl = incl64 - tiles_of<TL>(len64);
     const int n = __popcll(__ballot(first + lane < p.B && (base + excl) * (unsigned)units <= r.begin));
-    if (n == 0) break;
-    r.b = first + n - 1;
-    r.len = __builtin_amdgcn_readlane(len, n - 1);
-    r.before = base + (uint32_t)__builtin_amdgcn_readlane((int)excl, n - 1);
-    first += 64;
-    if (n < 64 || first >= p.B) break;
-    base += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
-    len = first + lane < p.B ? visible_keys(p, p.lens[first + lane]) : 0;
-    own = tiles_of<TL>(len);
-    incl = scan64(own);
+    if (n > 0) {
+      r.b = first + n - 1;
+      r.len = __builtin_amdgcn_readlane(len64, n - 1);
+      r.before = base + (uint32_t)__builtin_amdgcn_readlane((int)excl, n - 1);
+    }
+    base += (uint32_t)__builtin_amdgcn_readlane((int)incl64, 63);
+    return n == 64 && first + 64 < p.B;
+  };
+  bool more = true;
+#pragma unroll
+  for (int c = 0; c < HELD; ++c)
+    if (more) more = behind(64 * c, len[c], incl[c]);
+  for (int first = 64 * HELD; more; first += 64) {
+    const int next = first + lane < p.B ? visible_keys(p, p.lens[first + lane]) : 0;
+    more = behind(first, next, scan64(tiles_of<TL>(next)));
   }
   return r;
 }
@@ -144,7 +160,12 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   constexpr int LPT = TILEB / 1024, PIECE_ROWS = 1024 / ROWB;  // direct loads of a tile of keys or values, rows of one
   constexpr int LPB = LPT / NB > 0 ? LPT / NB : 1, RING = 2, NDB = D / 16, NKS = D / 32;
   static_assert(TILEB == 8192 && PIECE_ROWS <= 16 && LPB * NB == LPT, "a direct load stays inside a block of 16 keys");
-  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * RING * 2 * TILEB];
+  // The rows of q that a tile is the first to need come with it where they fit the LDS.  (Loaded to registers at the change, they are waited
+  // for behind all tiles requested before.  This kernel, us: 24 ragged sequences up to 1500 keys, 16 heads, d = 64 18.6 -> 17.7;
+  // 16 x 2000, 32/8 heads 27.0 -> 25.7; 32 ragged e4m3 sequences up to 9000, 64/8 heads 62.9 -> 61.3.)
+  constexpr bool QRING = NQ == 1;
+  constexpr int QB = QRING ? 32 * D : 0, QLOADS = QB / 1024;
+  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * RING * (2 * TILEB + QB)];
   LDS_AS char* const smem = (LDS_AS char*)smem_raw;
 
   const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, j16 = lane & 15, g = lane >> 4;
@@ -206,7 +227,18 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     koff[c] = r * ROWB + ((ch ^ attn_swz_k<ROWB>(r)) << 4);
     voff[c] = r * ROWB + ((ch ^ (FP8 ? attn_swz_k<ROWB>(r) : attn_swz_v<ROWB>(r))) << 4);
   }
+  uint32_t qoff[QRING ? QLOADS : 1];  // 16 query rows, chunks swizzled as the keys' (rows past the group's last re-read it)
+  if constexpr (QRING) {
+    constexpr int QCH = D / 8;
+#pragma unroll
+    for (int c = 0; c < QLOADS; ++c) {
+      const int r = c * (64 / QCH) + lane / QCH, ch = lane % QCH;
+      qoff[c] = min(r, G - 1) * (D * 2) + ((ch ^ attn_swz_k<D * 2>(r)) << 4);
+    }
+  }
   const uint32_t wave_base = w * (RING * 2 * TILEB), ring = (uint32_t)(uintptr_t)smem + wave_base;
+  const uint32_t q_base = kWaves * RING * 2 * TILEB + w * (RING * QB), q_ring = (uint32_t)(uintptr_t)smem + q_base;
+  bool ld_first = true;
   // Requests tile `ld` into `slot`; bit i of the result: block i has a page and a key.  A block that has none is read from where the tile
   // begins (or the cache's first rows) and hidden later.
   auto issue = [&](int slot) __attribute__((always_inline)) {
@@ -220,6 +252,14 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       ok |= has && j0 + 16 * i < ld.len ? 1u << i : 0u;
     }
     const uint32_t to = ring + slot * (2 * TILEB);
+    if constexpr (QRING) {
+      if (ld.t == 0 || ld_first) {
+        const char* const q_rows = (const char*)p.q + ((size_t)ld.b * p.Hq + (size_t)hk * G) * (D * 2);
+#pragma unroll
+        for (int c = 0; c < QLOADS; ++c) attn_lds_dma16(q_rows, qoff[c], q_ring + slot * QB + c * 1024);
+      }
+      ld_first = false;
+    }
 #pragma unroll
     for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.k + from[c / LPB], koff[c % LPB], to + c * 1024);
 #pragma unroll
@@ -248,16 +288,21 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   bf16x8 q[NQ][NKS];
   f32x4 o[NQ][NDB];
   float m[NQ], l[NQ];
-  auto start = [&]() __attribute__((always_inline)) {  // the rows of cp's unit
+  // features of step s that a lane holds, in chunks of 8
+  auto q_chunk = [&](int s) __attribute__((always_inline)) { return FP8 ? 8 * (s >> 1) + 2 * g + (s & 1) : 4 * s + g; };
+  auto start = [&](int slot) __attribute__((always_inline)) {  // the rows of cp's unit
     const int hk = cp.unit / QG, first = (cp.unit - hk * QG) * 16 * NQ;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-      const int h = first + 16 * i + j16;
-      const char* const src = (const char*)p.q + ((size_t)cp.b * p.Hq + (size_t)hk * G + h) * (D * 2);
+      if constexpr (QRING) {
 #pragma unroll
-      for (int s = 0; s < NKS; ++s) {
-        const int f = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-        q[i][s] = __builtin_bit_cast(bf16x8, h < G ? *(const u32x4*)(src + f * 2) : u32x4{0, 0, 0, 0});
+        for (int s = 0; s < NKS; ++s)
+          q[i][s] = __builtin_bit_cast(bf16x8, *(LDS_AS u32x4*)(smem + q_base + slot * QB + j16 * (D * 2) + ((q_chunk(s) ^ attn_swz_k<D * 2>(j16)) << 4)));
+      } else {
+        const int h = first + 16 * i + j16;
+        const char* const src = (const char*)p.q + ((size_t)cp.b * p.Hq + (size_t)hk * G + h) * (D * 2);
+#pragma unroll
+        for (int s = 0; s < NKS; ++s) q[i][s] = __builtin_bit_cast(bf16x8, h < G ? *(const u32x4*)(src + q_chunk(s) * 16) : u32x4{0, 0, 0, 0});
       }
 #pragma unroll
       for (int db = 0; db < NDB; ++db) o[i][db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -302,7 +347,8 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       }
     }
   };
-  // waits until at most N loads of this tile are under way (and those of the tile behind it, where one is requested)
+  // waits until at most N loads of this tile are under way (and those of the tile behind it, where one is requested: 2 LPT of them; with
+  // rows of q in front of it more, so that a few of its own are then waited for)
   auto wait = [&](auto value, bool behind) __attribute__((always_inline)) {
     constexpr int N = decltype(value)::value;
     if (behind) ATTN_WAIT_VMCNT(2 * LPT + N);
@@ -312,8 +358,9 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   };
 
   uint32_t have = 0;  // NB bits for each tile in the ring
-  start();
   int began = cp.t, slot = 0, part = 0;
+  bool fresh = true;
+  if constexpr (!QRING) start(0);
   for (int i = 0; i < min(n, RING); ++i) {
     have |= issue(i) << (NB * i);
     if (i + 1 < n) {
@@ -325,6 +372,10 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     const int base = slot * (2 * TILEB);
     const bool behind = i + 1 < n;
     wait(std::integral_constant<int, LPT>{}, behind);
+    if constexpr (QRING) {
+      if (fresh) start(slot);
+      fresh = false;
+    }
 
     // visible rows of the tile's blocks
     const int keys = cp.len - (cp.t << TL);
@@ -438,7 +489,8 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       part = 1;
       if (i + 1 < n) {
         advance(cp);
-        start();
+        if constexpr (!QRING) start(0);
+        fresh = true;
         began = 0;
       }
     } else {
@@ -447,37 +499,30 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   }
 }
 
-// Joins what the waves left of the (sequence, key head) pairs that more than one of them took, and writes the rows of sequences
-// without keys.  WAVES waves for a query row: one, or, where there are few rows, each with many parts, sixteen.
-template <int D, int WAVES>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(const DecodeParams p, int NQ, int tile_log2) {
-  constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, parts a wave takes side by side and requests in a row
-  const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int row = WAVES == 1 ? blockIdx.x * 4 + w : blockIdx.x;
-  if (row >= p.B * p.Hq) return;  // (WAVES 1: no barrier follows)
+// Joins what the waves left of a (sequence, unit) that more than one of them took, or writes the rows of a sequence without keys; one
+// workgroup for each.  D / 4 lanes take a row.  Few parts: they take them one after the other, four requested at a time, and the workgroup's
+// lanes hold different rows; many (MANY): different parts of a row are shared out, over a whole workgroup of sixteen waves for each row.
+template <int D, bool MANY>
+__global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const DecodeParams p, int NQ, int tile_log2) {
+  constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, rows (MANY: parts) a wave holds side by side
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG, kept = rows_kept(G);
-  const int b = row / p.Hq, hq = row - b * p.Hq, hk = hq / G, qg = (hq - hk * G) / (16 * NQ), r = hq - hk * G - qg * 16 * NQ;
-  const int* const split = (const int*)((const char*)p.ws + split_offset(kept, D)) + ((size_t)b * units + hk * QG + qg) * 4;
+  const int segment = MANY ? blockIdx.x / kept : blockIdx.x, b = segment / units, unit = segment - b * units;
+  const int* const split = (const int*)((const char*)p.ws + split_offset(kept, D)) + (size_t)segment * 4;
   const int len = visible_keys(p, scalar_load(p.lens, b));
   const int split_first = scalar_load(split, 0), w1 = scalar_load(split, 1), all = scalar_load(split, 2);
-  const size_t out = (size_t)row * D;
-  if (len == 0) {  // (nothing was written for it)
-    if (w == 0 || WAVES == 1) {
-      for (int i = lane; i < D / 2; i += 64) ((uint32_t*)p.o)[out / 2 + i] = 0;
-      if (lane == 0) p.lse[row] = -__builtin_inff();
-    }
-    return;
-  }
-  if (split_first < 0) return;
+  if (len > 0 && split_first < 0) return;  // one wave took it all
+  const int lane = threadIdx.x & 63, w = uniform((int)(threadIdx.x >> 6)), sub = lane / LPR, col = (lane % LPR) * 4;
+  const int hk = unit / QG, first_row = (unit - hk * QG) * 16 * NQ, rows = min(kept, G - first_row);
+  const size_t out = (size_t)b * p.Hq + (size_t)hk * G + first_row;
+
   // (kept inside the workspace whatever it holds: `lens` may have changed under the call)
   const int first_sum = min(split_first, 2 * kWorkers - 1), w0 = first_sum >> 1, stride = partial_floats(kept, D);
-  // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile
-  const int parts = min(all ? (len + (1 << tile_log2) - 1) >> tile_log2 : w1 - w0 + 1, kWorkers - w0);
+  // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile; without keys there is none
+  const int parts = len == 0 ? 0 : min(all ? (len + (1 << tile_log2) - 1) >> tile_log2 : w1 - w0 + 1, kWorkers - w0);
   const uint32_t first = all ? ((uint32_t)all * (uint32_t)w0) >> kWorkersLog2 : 0;
 
-  const int sub = lane / LPR, col = (lane % LPR) * 4;
-  float m = -__builtin_inff(), l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  f32x4 o;
+  float m, l;
   auto merge = [&](float om, float ol, const f32x4& oo) __attribute__((always_inline)) {
     const float m_new = fmaxf(m, om), ref = m_new == -__builtin_inff() ? 0.f : m_new;
     const float a = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2), c = __builtin_amdgcn_exp2f((om - ref) * p.scale_log2);
@@ -485,32 +530,52 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(
     l = l * a + ol * c;
     m = m_new;
   };
-  for (int i0 = (WAVES == 1 ? 0 : w * PER * AT_ONCE) + sub; i0 < parts; i0 += PER * AT_ONCE * WAVES) {
-    f32x4 po[AT_ONCE];
-    float pm[AT_ONCE], pl[AT_ONCE];
+  // parts i0, i0 + step, ... of row r
+  auto add_parts = [&](int r, int i0, int step, int rounds) __attribute__((always_inline)) {
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -__builtin_inff();
+    l = 0.f;
+    for (int at = i0; at < parts; at += rounds) {
+      f32x4 po[AT_ONCE];
+      float pm[AT_ONCE], pl[AT_ONCE];
 #pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) {
-      const int i = min(i0 + k * PER, parts - 1);
-      const int x = all ? (int)((((first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all) : w0 + i;
-      const float* const src = (const float*)p.ws + (size_t)(i == 0 ? first_sum : min(2 * x, 2 * kWorkers - 1)) * stride;
-      po[k] = *(const f32x4*)(src + r * D + col);
-      pm[k] = src[kept * D + 2 * r];
-      pl[k] = src[kept * D + 2 * r + 1];
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const int i = min(at + k * step, parts - 1);
+        const int x = all ? (int)((((first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all) : w0 + i;
+        const float* const src = (const float*)p.ws + (size_t)(i == 0 ? first_sum : min(2 * x, 2 * kWorkers - 1)) * stride;
+        po[k] = *(const f32x4*)(src + r * D + col);
+        pm[k] = src[kept * D + 2 * r];
+        pl[k] = src[kept * D + 2 * r + 1];
+      }
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k)
+        if (at + k * step < parts) merge(pm[k], pl[k], po[k]);
     }
+  };
+  auto write = [&](int r) __attribute__((always_inline)) {
+    const float inv = l == 0.f ? 0.f : p.out_scale / l;
+    *(u32x2*)((char*)p.o + ((out + r) * D + col) * 2) = u32x2{attn_pack_bf16(o[0] * inv, o[1] * inv), attn_pack_bf16(o[2] * inv, o[3] * inv)};
+    if (col == 0) p.lse[out + r] = l == 0.f ? -__builtin_inff() : (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * kLn2;
+  };
+
+  if constexpr (!MANY) {
+    for (int r = w * PER + sub; r < rows; r += blockDim.x / LPR) {
+      add_parts(r, 0, 1, AT_ONCE);
+      write(r);
+    }
+  } else {
+    __shared__ float so[16][D], sm[16], sl[16];
+    const int r = blockIdx.x - segment * kept;
+    if (r >= rows) return;
+    add_parts(r, w * PER * AT_ONCE + sub, PER, 16 * PER * AT_ONCE);
 #pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k)
-      if (i0 + k * PER < parts) merge(pm[k], pl[k], po[k]);
-  }
+    for (int k = LPR; k < 64; k *= 2) {
+      const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
+      f32x4 oo;
 #pragma unroll
-  for (int k = LPR; k < 64; k *= 2) {
-    const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
-    f32x4 oo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) oo[i] = __shfl_xor(o[i], k);
-    merge(om, ol, oo);
-  }
-  if constexpr (WAVES > 1) {
-    __shared__ float so[WAVES][D], sm[WAVES], sl[WAVES];
+      for (int i = 0; i < 4; ++i) oo[i] = __shfl_xor(o[i], k);
+      merge(om, ol, oo);
+    }
     if (sub == 0) *(f32x4*)&so[w][col] = o;
     if (lane == 0) {
       sm[w] = m;
@@ -518,12 +583,9 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) kv_join_kernel(
     }
     __syncthreads();
     if (w != 0) return;
-    for (int k = 1; k < min(WAVES, (parts + PER * AT_ONCE - 1) / (PER * AT_ONCE)); ++k) merge(sm[k], sl[k], *(const f32x4*)&so[k][col]);
+    for (int k = 1; k < min(16, (parts + PER * AT_ONCE - 1) / (PER * AT_ONCE)); ++k) merge(sm[k], sl[k], *(const f32x4*)&so[k][col]);
+    if (sub == 0) write(r);
   }
-  if (sub != 0) return;
-  const float inv = l == 0.f ? 0.f : p.out_scale / l;
-  *(u32x2*)((char*)p.o + (out + col) * 2) = u32x2{attn_pack_bf16(o[0] * inv, o[1] * inv), attn_pack_bf16(o[2] * inv, o[3] * inv)};
-  if (lane == 0) p.lse[row] = l == 0.f ? -__builtin_inff() : (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <int D, bool FP8>
@@ -536,10 +598,14 @@ void launch_decode(const DecodeParams& p, int nq, hipStream_t stream) {
 
 template <int D>
 void launch_join(const DecodeParams& p, int nq, int tile_log2, hipStream_t stream) {
-  const int rows = p.B * p.Hq, G = p.Hq / p.Hkv;
-  // 1024 waves leave about 1024 / (sequences x units) parts of each; one wave takes 8 (d = 64: 16) at a time
-  if ((long long)p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq)) < 64) kv_join_kernel<D, 16><<<rows, 1024, 0, stream>>>(p, nq, tile_log2);
-  else kv_join_kernel<D, 1><<<(rows + 3) / 4, 256, 0, stream>>>(p, nq, tile_log2);
+  const int G = p.Hq / p.Hkv, segments = p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq)), kept = rows_kept(G);
+  // 1024 waves leave about 1024 / segments parts of each
+  if (segments < 64) {
+    kv_join_kernel<D, true><<<segments * kept, 1024, 0, stream>>>(p, nq, tile_log2);
+  } else {
+    const int rows_per_wave = 256 / D, waves = (kept + rows_per_wave - 1) / rows_per_wave;
+    kv_join_kernel<D, false><<<segments, 64 * (waves < 4 ? waves : 4), 0, stream>>>(p, nq, tile_log2);
+  }
 }
 
 }  // namespace
