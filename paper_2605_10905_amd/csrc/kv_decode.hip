@@ -7,7 +7,8 @@
 // key head; each of kWorkers waves takes an equal, consecutive piece of it, whatever the lengths are.  What the pieces are follows from
 // `lens` on the device, by a scan over them that every wave does for itself.  A wave that covers all tiles of a (sequence, key head) writes its
 // rows of o; a wave that covers some of them leaves its sums (32 bits) in the workspace, at most two per wave (where its piece begins and
-// where it ends), and the second kernel joins them.
+// where it ends), and the second kernel joins them.  Where the four waves of a workgroup work on one (sequence, key head) alone, they add
+// their sums in LDS first.
 //
 // A wave streams its tiles through a ring of its own in LDS (two of 16 KB: 128 KB of a CU's four waves, of which at least half is in
 // flight), by direct-to-LDS loads, so that no barrier is needed anywhere.  Page entries come through the scalar cache, whose counter is
@@ -149,11 +150,12 @@ struct Split {
   int first;  // 2 * wave + which of its two sums the first part is; -1: one wave took it all
   int last;   // the wave of the last part
   int all;    // tiles of the whole list where there are fewer than waves (a wave then has one of them at most), else 0
-  int unused;
+  int ends;   // (with last) whether that wave's piece ends with this (sequence, unit)
 };
 __host__ __device__ __forceinline__ size_t split_offset(int rows, int d) { return (size_t)2 * kWorkers * partial_floats(rows, d) * sizeof(float); }
 
-template <int D, bool FP8, int NQ>
+// JOINT: whether a workgroup's waves add their sums where they can (see the end).
+template <int D, bool FP8, int NQ, bool JOINT>
 __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeParams p) {
   constexpr int ROWB = D * (FP8 ? 1 : 2), NCH = ROWB / 16, TL = kTileLog2<ROWB>, KT = 1 << TL, TILEB = KT * ROWB;
   constexpr int NB = KT / 16, NP = KT / 32;                    // blocks of 16 keys, pairs of them
@@ -165,7 +167,8 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   // 16 x 2000, 32/8 heads 27.0 -> 25.7; 32 ragged e4m3 sequences up to 9000, 64/8 heads 62.9 -> 61.3.)
   constexpr bool QRING = NQ == 1;
   constexpr int QB = QRING ? 32 * D : 0, QLOADS = QB / 1024;
-  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * RING * (2 * TILEB + QB)];
+  constexpr int STATB = QRING ? RING * QB : NQ * 16 * 8;  // at the end: (maximum, sum) of the wave's rows
+  __shared__ __attribute__((aligned(1024))) char smem_raw[kWaves * (RING * 2 * TILEB + STATB)];
   LDS_AS char* const smem = (LDS_AS char*)smem_raw;
 
   const int w = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, j16 = lane & 15, g = lane >> 4;
@@ -174,7 +177,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   const int page_mask = (1 << p.page_log2) - 1;
 
   const Piece at = piece_of<TL>(p, worker, units);
-  if (at.begin == at.end) return;
+  if (at.begin == at.end) return;  // (fewer tiles than waves: there is no barrier below then)
   const int n = (int)(at.end - at.begin);  // (2^10 waves share far below 2^41 tiles: a cache fits the memory)
 
   // A position in the list: tile t of `unit` of sequence b, and the page entries of its blocks
@@ -311,18 +314,23 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     }
   };
   const int kept = rows_kept(G);
-  auto finish = [&](bool head, bool tail, int part) __attribute__((always_inline)) {  // (with the first tile, with the last)
+  // what the second kernel has to know, by the wave with the first tile (head) and the one with the last (tail)
+  auto record = [&](bool head, bool tail, bool whole, int part, bool ends) __attribute__((always_inline)) {
+    if (lane != 0 || !(head || tail)) return;
+    Split* const x = (Split*)((char*)p.ws + split_offset(kept, D)) + ((size_t)cp.b * units + cp.unit);
+    if (head) {
+      x->first = whole ? -1 : 2 * worker + part;
+      x->all = at.all < kWorkers ? (int)at.all : 0;
+    }
+    if (tail && !whole) {
+      x->last = worker;
+      x->ends = ends ? 1 : 0;
+    }
+  };
+  auto finish = [&](bool head, bool tail, int part, bool ends) __attribute__((always_inline)) {  // (with the first tile, with the last)
     const int hk = cp.unit / QG, first = (cp.unit - hk * QG) * 16 * NQ;
     const bool whole = head && tail;
-    if (lane == 0 && (head || tail)) {
-      Split* const x = (Split*)((char*)p.ws + split_offset(kept, D)) + ((size_t)cp.b * units + cp.unit);
-      if (head) {
-        x->first = whole ? -1 : 2 * worker + part;
-        x->all = at.all < kWorkers ? (int)at.all : 0;
-      } else {
-        x->last = worker;
-      }
-    }
+    record(head, tail, whole, part, ends);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int r = 16 * i + j16;
@@ -484,8 +492,9 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     slot ^= 1;
 
     const bool last = cp.t + 1 == cp.nt;
+    if (JOINT && i + 1 == n) break;
     if (last || i + 1 == n) {
-      finish(began == 0, last, part);
+      finish(began == 0, last, part, i + 1 == n);
       part = 1;
       if (i + 1 < n) {
         advance(cp);
@@ -497,12 +506,75 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       ++cp.t;
     }
   }
+  if constexpr (!JOINT) return;
+
+  // Whether the pieces of the workgroup's waves lie in this (sequence, unit): then all of them find so, and add their sums.
+  const unsigned long long seg_begin = at.end - 1 - (unsigned)cp.t, seg_end = seg_begin + (unsigned)cp.nt;
+  const unsigned long long wg_begin = (at.all * (unsigned)(worker - w)) >> kWorkersLog2, wg_end = (at.all * (unsigned)(worker - w + kWaves)) >> kWorkersLog2;
+  if (at.all < kWorkers || wg_begin < seg_begin || seg_end < wg_end) {
+    finish(began == 0, cp.t + 1 == cp.nt, part, true);
+    return;
+  }
+
+  // The workgroup's sums: every wave leaves its own in its ring and adds a quarter of the blocks of all four, in the waves' order: four times
+  // fewer parts to write, read and join.
+  const bool head = seg_begin == wg_begin, tail = wg_end == seg_end, whole = head && tail;
+  record(head && w == 0, tail && w == kWaves - 1, whole, 0, true);
+  auto stat = [&](int wave) __attribute__((always_inline)) { return (LDS_AS float*)(smem + kWaves * RING * 2 * TILEB + wave * STATB); };
+  auto block = [&](int wave, int x) __attribute__((always_inline)) { return (LDS_AS f32x4*)(smem + wave * (RING * 2 * TILEB) + (x * 64 + lane) * 16); };
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const float sum = sum_rows(l[i]);
+    if (g == 0) {
+      stat(w)[2 * (16 * i + j16)] = m[i];
+      stat(w)[2 * (16 * i + j16) + 1] = sum;
+    }
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) *block(w, i * NDB + db) = o[i][db];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    float wm[kWaves], mx = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      wm[k] = stat(k)[2 * (16 * i + j16)];
+      mx = fmaxf(mx, wm[k]);
+    }
+    const float ref = mx == -__builtin_inff() ? 0.f : mx;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      wm[k] = __builtin_amdgcn_exp2f((wm[k] - ref) * p.scale_log2);
+      sum += wm[k] * stat(k)[2 * (16 * i + j16) + 1];
+    }
+    const int hk = cp.unit / QG, first = (cp.unit - hk * QG) * 16 * NQ, r = 16 * i + j16;
+    const size_t row = (size_t)cp.b * p.Hq + (size_t)hk * G + first + r;
+    const float inv = sum == 0.f ? 0.f : p.out_scale / sum;
+    float* const dst = (float*)p.ws + (size_t)(2 * (worker - w)) * partial_floats(kept, D);
+#pragma unroll
+    for (int d0 = 0; d0 < NDB; d0 += kWaves) {
+      const int db = d0 + w;
+      f32x4 val = *block(0, i * NDB + db) * wm[0];
+#pragma unroll
+      for (int k = 1; k < kWaves; ++k) val += *block(k, i * NDB + db) * wm[k];
+      if (first + r >= G) continue;
+      if (whole) *(u32x2*)((char*)p.o + row * (D * 2) + db * 32 + g * 8) = u32x2{attn_pack_bf16(val[0] * inv, val[1] * inv), attn_pack_bf16(val[2] * inv, val[3] * inv)};
+      else *(f32x4*)(dst + r * D + db * 16 + g * 4) = val;
+    }
+    if (w != 0 || g != 0 || first + r >= G) continue;
+    if (whole) {
+      p.lse[row] = sum == 0.f ? -__builtin_inff() : (mx * p.scale_log2 + __builtin_amdgcn_logf(sum)) * kLn2;
+    } else {
+      dst[kept * D + 2 * r] = mx;
+      dst[kept * D + 2 * r + 1] = sum;
+    }
+  }
 }
 
 // Joins what the waves left of a (sequence, unit) that more than one of them took, or writes the rows of a sequence without keys; one
 // workgroup for each.  D / 4 lanes take a row.  Few parts: they take them one after the other, four requested at a time, and the workgroup's
 // lanes hold different rows; many (MANY): different parts of a row are shared out, over a whole workgroup of sixteen waves for each row.
-template <int D, bool MANY>
+template <int D, bool MANY, bool JOINT>
 __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const DecodeParams p, int NQ, int tile_log2) {
   constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, rows (MANY: parts) a wave holds side by side
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG, kept = rows_kept(G);
@@ -510,6 +582,7 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
   const int* const split = (const int*)((const char*)p.ws + split_offset(kept, D)) + (size_t)segment * 4;
   const int len = visible_keys(p, scalar_load(p.lens, b));
   const int split_first = scalar_load(split, 0), w1 = scalar_load(split, 1), all = scalar_load(split, 2);
+  const int ends = JOINT ? scalar_load(split, 3) : 0;
   if (len > 0 && split_first < 0) return;  // one wave took it all
   const int lane = threadIdx.x & 63, w = uniform((int)(threadIdx.x >> 6)), sub = lane / LPR, col = (lane % LPR) * 4;
   const int hk = unit / QG, first_row = (unit - hk * QG) * 16 * NQ, rows = min(kept, G - first_row);
@@ -517,9 +590,19 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
 
   // (kept inside the workspace whatever it holds: `lens` may have changed under the call)
   const int first_sum = min(split_first, 2 * kWorkers - 1), w0 = first_sum >> 1, stride = partial_floats(kept, D);
-  // every wave from w0 to w1 has a part, or, where there are fewer tiles than waves, the one of each tile; without keys there is none
-  const int parts = len == 0 ? 0 : min(all ? (len + (1 << tile_log2) - 1) >> tile_log2 : w1 - w0 + 1, kWorkers - w0);
+  // The parts: of every wave from w0 to w1, but one of each workgroup whose four waves work on nothing else (groups g0 to g1); or, where there
+  // are fewer tiles than waves, of the wave of each tile; without keys there is none.
   const uint32_t first = all ? ((uint32_t)all * (uint32_t)w0) >> kWorkersLog2 : 0;
+  const int g0 = (w0 + (first_sum & 1) + kWaves - 1) / kWaves, g1 = (w1 + (ends ? 1 : 0)) / kWaves - 1, groups = !JOINT || all ? 0 : max(g1 - g0 + 1, 0);
+  const int front = groups ? kWaves * g0 - w0 : kWorkers;
+  int parts = all ? (len + (1 << tile_log2) - 1) >> tile_log2 : w1 - w0 + 1 - (kWaves - 1) * groups;
+  parts = len == 0 ? 0 : min(parts, kWorkers);
+  auto sums_of = [&](int i) __attribute__((always_inline)) {  // which of the 2 * kWorkers sums part i is
+    if (i == 0) return first_sum;
+    const int x = all ? (int)((((first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all)
+                  : !JOINT || i < front ? w0 + i : i < front + groups ? kWaves * (g0 + i - front) : w0 + i + (kWaves - 1) * groups;
+    return min(2 * x, 2 * kWorkers - 1);
+  };
 
   f32x4 o;
   float m, l;
@@ -540,9 +623,7 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
       float pm[AT_ONCE], pl[AT_ONCE];
 #pragma unroll
       for (int k = 0; k < AT_ONCE; ++k) {
-        const int i = min(at + k * step, parts - 1);
-        const int x = all ? (int)((((first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all) : w0 + i;
-        const float* const src = (const float*)p.ws + (size_t)(i == 0 ? first_sum : min(2 * x, 2 * kWorkers - 1)) * stride;
+        const float* const src = (const float*)p.ws + (size_t)sums_of(min(at + k * step, parts - 1)) * stride;
         po[k] = *(const f32x4*)(src + r * D + col);
         pm[k] = src[kept * D + 2 * r];
         pl[k] = src[kept * D + 2 * r + 1];
@@ -588,39 +669,51 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
   }
 }
 
-template <int D, bool FP8>
+// Workgroups add their sums where there are few enough (sequence, unit) pairs, on average two workgroups or more to each.  us, apart / added:
+// 64 x 4000 keys, 64/1 heads 61.2 / 44.8, 32/1 41.2 / 32.9; 128 x 4000, 32/2 heads 100 / 95; 1 x 131072 e4m3, 8/1 heads 23.1 / 17.3; 2 x 131072,
+// 64/8 heads 191.9 / 190.2.  Where it is seldom possible the code for it costs: 211 ragged sequences up to 140 keys, 32/4 heads 17.5 / 18.2;
+// 71 up to 1894, e4m3, 56/8 heads 23.8 / 24.3.
+bool sums_are_added(long long segments) { return segments <= 128; }
+
+template <int D, bool FP8, bool JOINT>
 void launch_decode(const DecodeParams& p, int nq, hipStream_t stream) {
   constexpr int grid = kWorkers / kWaves;
-  if (nq == 1) kv_decode_kernel<D, FP8, 1><<<grid, kWaves * 64, 0, stream>>>(p);
-  else if (nq == 2) kv_decode_kernel<D, FP8, 2><<<grid, kWaves * 64, 0, stream>>>(p);
-  else kv_decode_kernel<D, FP8, 4><<<grid, kWaves * 64, 0, stream>>>(p);
+  if (nq == 1) kv_decode_kernel<D, FP8, 1, JOINT><<<grid, kWaves * 64, 0, stream>>>(p);
+  else if (nq == 2) kv_decode_kernel<D, FP8, 2, JOINT><<<grid, kWaves * 64, 0, stream>>>(p);
+  else kv_decode_kernel<D, FP8, 4, JOINT><<<grid, kWaves * 64, 0, stream>>>(p);
 }
 
-template <int D>
-void launch_join(const DecodeParams& p, int nq, int tile_log2, hipStream_t stream) {
-  const int G = p.Hq / p.Hkv, segments = p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq)), kept = rows_kept(G);
-  // 1024 waves leave about 1024 / segments parts of each
-  if (segments < 64) {
-    kv_join_kernel<D, true><<<segments * kept, 1024, 0, stream>>>(p, nq, tile_log2);
-  } else {
-    const int rows_per_wave = 256 / D, waves = (kept + rows_per_wave - 1) / rows_per_wave;
-    kv_join_kernel<D, false><<<segments, 64 * (waves < 4 ? waves : 4), 0, stream>>>(p, nq, tile_log2);
+template <int D, bool JOINT>
+void launch_join(const DecodeParams& p, int nq, int segments, int tile_log2, hipStream_t stream) {
+  const int kept = rows_kept(p.Hq / p.Hkv), rows_per_wave = 256 / D, waves = (kept + rows_per_wave - 1) / rows_per_wave;
+  // up to 256 / segments parts and six more of each, where there are fewer tiles than waves up to 1024 / segments
+  if constexpr (JOINT) {
+    if (segments < 64) {
+      kv_join_kernel<D, true, true><<<segments * kept, 1024, 0, stream>>>(p, nq, tile_log2);
+      return;
+    }
   }
+  kv_join_kernel<D, false, JOINT><<<segments, 64 * (waves < 4 ? waves : 4), 0, stream>>>(p, nq, tile_log2);
+}
+
+template <bool JOINT>
+int launch(const DecodeParams& p, int d, bool fp8, int nq, int segments, hipStream_t stream) {
+  if (d == 128 && fp8) launch_decode<128, true, JOINT>(p, nq, stream);
+  else if (d == 128) launch_decode<128, false, JOINT>(p, nq, stream);
+  else if (fp8) launch_decode<64, true, JOINT>(p, nq, stream);
+  else launch_decode<64, false, JOINT>(p, nq, stream);
+  if (hipGetLastError() != hipSuccess) return 1;
+  const int tile_log2 = d == 128 && !fp8 ? kTileLog2<256> : d == 64 && fp8 ? kTileLog2<64> : kTileLog2<128>;
+  if (d == 128) launch_join<128, JOINT>(p, nq, segments, tile_log2, stream);
+  else launch_join<64, JOINT>(p, nq, segments, tile_log2, stream);
+  return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
 }  // namespace
 
 int kv_decode_launch(const DecodeParams& p, int d, bool fp8, hipStream_t stream) {
-  const int nq = blocks_for(p.Hq / p.Hkv);
-  if (d == 128 && fp8) launch_decode<128, true>(p, nq, stream);
-  else if (d == 128) launch_decode<128, false>(p, nq, stream);
-  else if (fp8) launch_decode<64, true>(p, nq, stream);
-  else launch_decode<64, false>(p, nq, stream);
-  if (hipGetLastError() != hipSuccess) return 1;
-  const int tile_log2 = d == 128 && !fp8 ? kTileLog2<256> : d == 64 && fp8 ? kTileLog2<64> : kTileLog2<128>;
-  if (d == 128) launch_join<128>(p, nq, tile_log2, stream);
-  else launch_join<64>(p, nq, tile_log2, stream);
-  return hipGetLastError() == hipSuccess ? 0 : 1;
+  const int G = p.Hq / p.Hkv, nq = blocks_for(G), segments = p.B * p.Hkv * ((G + 16 * nq - 1) / (16 * nq));  // (B * Hq fits 24 bits)
+  return sums_are_added(segments) ? launch<true>(p, d, fp8, nq, segments, stream) : launch<false>(p, d, fp8, nq, segments, stream);
 }
 
 long long kv_decode_bytes(int B, int Hq, int Hkv, int d) {

@@ -180,6 +180,45 @@ def test_positions_outside_the_table_are_nan_and_nothing_else():
     assert bool(rows[good].isfinite().all()) and bool(rows[:, Hq + Hkv:].isfinite().all())
 
 
+def test_rope_of_more_tokens_than_a_launch_has_waves_for():
+    """12 million tokens of three heads: more than 2^31 elements and 2^32 bytes, and more tasks than workgroups start; rows at both ends and between."""
+    A = _A()
+    N, d, npos = 12_000_000, 64, 90
+    gen = ku.generator(9)
+    width, w, tab = 3 * d, ku.weights(gen, d, True), ku.table(npos, d)
+    qkv = torch.empty((N, width), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, N, 1_000_000):
+        qkv[i:i + 1_000_000] = torch.randn((min(1_000_000, N - i), width), generator=gen, device="cuda").bfloat16()
+    pos = torch.randint(0, npos, (N,), generator=gen, device="cuda", dtype=torch.int32)
+    outs = [torch.full((1, 1, N, d), NAN, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    A.rope_qkv(qkv, width, *w, EPS, tab, npos, d, False, pos, *outs, 1, 1, 1, N, d)
+    torch.cuda.synchronize()
+    assert all(bool(o.isfinite().all()) for o in outs) and torch.equal(outs[2][0, 0], qkv[:, 2 * d:])
+    at = torch.cat([torch.arange(50), torch.randint(0, N, (300,), generator=torch.Generator().manual_seed(3)), torch.arange(N - 50, N)]).cuda()
+    x, p = f64(qkv[at]).reshape(-1, 3, d), pos[at].cpu().tolist()
+    args = (1, 1, *map(ku.arr, w), EPS, _host_table(tab), p, d, False)
+    want, plain = orc.rope_qkv(x, *args), orc.rope_qkv(x, *args[:-2], 0, False)
+    for o, ref, y in zip(outs[:2], want, plain):
+        assert (np.abs(f64(o[0, 0, at])[:, None] - ref) <= ku.forward_bound(ref, ku.row_size(y))).all()
+    dqkv, dw = torch.full_like(qkv, NAN), [torch.empty(d, device="cuda") for _ in range(2)]
+    ws = torch.empty(A.rope_qkv_bwd_workspace_bytes(1, 1, 1, N, d) // 4, device="cuda")
+    A.rope_qkv_bwd(*outs, qkv, width, *w, EPS, tab, npos, d, False, pos, dqkv, width, *dw, ws, 1, 1, 1, N, d)
+    torch.cuda.synchronize()
+    assert bool(dqkv.isfinite().all()) and torch.equal(dqkv[:, 2 * d:], qkv[:, 2 * d:])
+    g = [f64(o[0, 0, at])[:, None] for o in outs]
+    ref, _, _ = orc.rope_qkv_bwd(*g, x, *args)
+    for h, wt in enumerate(w):  # (the bound of test_rope_qkv_bwd)
+        n = orc.rms(x[:, h:h + 1], EPS)
+        size = 2 * ku.row_size(g[h]) * np.abs(ku.arr(wt)).max() / n * (1 + (ku.row_size(x[:, h:h + 1]) / n) ** 2)
+        got = f64(dqkv[at]).reshape(-1, 3, d)[:, h:h + 1]
+        assert (np.abs(got - ref[:, h:h + 1]) <= 2.0 ** -8 * np.abs(ref[:, h:h + 1]) * (1 + 2.0 ** -8) + 2.0 ** -18 * size + 1e-38).all()
+    # q's gradient is its output here, and rotations keep lengths: the weight's gradient is w_i times the sum of xhat_i^2 mixed over the pair;
+    # summed over all features with those weights, sum_i w_i dw_i = sum of |y|^2 = sum of |z|^2
+    for o, wt, got in zip(outs, w, dw):
+        total = float(sum(o[0, 0, i:i + 1_000_000].double().square().sum() for i in range(0, N, 1_000_000)))
+        assert abs(float((got.double() * wt.double()).sum()) - total) <= 2.0 ** -8 * total  # (z rounded to bf16)
+
+
 # ---- kv_append ---------------------------------------------------------------------------------
 
 APPEND = [
@@ -332,6 +371,24 @@ def test_kv_decode_splits(lens, Hq, Hkv, d, fp8):
     q = _q(gen, len(lens), Hq, d)
     o, lse = _decode(q, cache, 0.11)
     ku.decode_check(o, lse, q, cache, 0.11)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d,fp8", [
+    ([128] * 32, 16, 8, 128, False),         # as many (sequence, key head) pairs as workgroups: each of them takes one whole
+    ([256] * 64, 20, 4, 64, False), ([257] * 32, 8, 8, 128, True), ([100] * 300, 3, 1, 128, False),
+    ([70000], 8, 1, 128, False), ([70001], 64, 1, 64, True), ([33000, 33000], 70, 2, 128, False), ([16001, 7, 0, 40000], 33, 1, 128, True),
+    ([4000] * 20 + [1] * 9, 32, 1, 64, False), ([999] * 40, 64, 1, 128, True), ([50000, 64], 16, 2, 64, False), ([32768], 4, 1, 128, False),
+    ([32 * 1023], 4, 1, 128, False), ([32 * 1025], 4, 1, 128, False), ([32 * 1028, 32 * 4], 5, 1, 128, False),
+], ids=lambda x: f"{len(x)}x{max(x)}" if isinstance(x, list) else str(x))
+def test_kv_decode_pieces_that_share_a_workgroup(lens, Hq, Hkv, d, fp8):
+    """Pieces of the work that begin and end with a workgroup's and that do not: sums of four waves, of one, of all."""
+    gen = ku.generator(65 + len(lens))
+    cache = ku.Cache(gen, lens, Hkv, d, 64, fp8)
+    q = _q(gen, len(lens), Hq, d)
+    o, lse = _decode(q, cache, d ** -0.5)
+    ku.decode_check(o, lse, q, cache, d ** -0.5)
+    o2, lse2 = _decode(q, cache, d ** -0.5)
+    assert torch.equal(o.view(torch.int16), o2.view(torch.int16)) and torch.equal(lse, lse2)
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -503,6 +560,18 @@ def test_tensors_of_another_device_are_refused():
     call, t = importlib.import_module("paper_2605_10905_amd.kv")._call, torch.zeros(64, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(ValueError, match="q is on device 0, the current one is 1"):
         call.kv_decode(1, 0, t, *[4096] * 7, 1, 1, 1, 64, 1, 16, 1, 1.0, 0, 1.0, 1.0)
+
+
+@pytest.mark.parametrize("d,fp8", [(64, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("G", [3, 20, 50, 70])
+def test_kv_decode_many_pairs(G, d, fp8):
+    """More (sequence, key head) pairs than workgroups share: every number of query blocks, every type."""
+    gen = ku.generator(67 + G)
+    lens = [(53 * i) % 300 for i in range(150)]
+    cache = ku.Cache(gen, lens, 1, d, 32, fp8)
+    q = _q(gen, len(lens), G, d)
+    o, lse = _decode(q, cache, d ** -0.5)
+    ku.decode_check(o, lse, q, cache, d ** -0.5)
 
 
 # ---- together ----------------------------------------------------------------------------------

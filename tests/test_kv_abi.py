@@ -194,10 +194,9 @@ def _all_calls():
             calls += [("rope_qkv", dict(rope, q=P, k=P, v=P, **size)),
                       ("rope_qkv_bwd", dict(rope, dq=P, dk=P, dv=P, dqkv=P, dld=16 * d, dq_weight=w, dk_weight=w, workspace=w, **size))]
             calls += [("kv_append", dict(rope, seq=P, pages=P, q=P, k_cache=P, v_cache=P, T=4, S=4, Hq=2, Hkv=1, d=d, W=2, page_size=16, num_pages=9, dtype=t)) for t in (0, 1)]
-        calls += [("kv_decode", dict(q=P, k_cache=P, v_cache=P, pages=P, lens=P, o=P, lse=P, workspace=P, B=2, Hq=G * 2, Hkv=2, d=d, W=2, page_size=16, num_pages=9,
-                                     scale=0.1, dtype=t)) for t in (0, 1) for G in (1, 5, 16, 17, 32, 33, 65)]
-        # (many rows: one wave joins a row)
-        calls += [("kv_decode", dict(calls[-1][1], B=1500, Hq=2, Hkv=1))]
+        # few and many (sequence, key head) pairs: 2, 100 and 200 of them, more with many heads to one
+        calls += [("kv_decode", dict(q=P, k_cache=P, v_cache=P, pages=P, lens=P, o=P, lse=P, workspace=P, B=B, Hq=G, Hkv=1, d=d, W=2, page_size=16, num_pages=9,
+                                     scale=0.1, dtype=t)) for t in (0, 1) for G in (1, 5, 16, 17, 32, 33, 65) for B in (2, 100, 200)]
     return calls
 
 
