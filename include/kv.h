@@ -82,8 +82,9 @@ long long rope_qkv_bwd_workspace_bytes(int B, int Hq, int Hkv, int N, int d);
 /*
  * The paged cache: k_cache and v_cache are [num_pages, Hkv, page_size, d] each, bfloat16 (ATTN_BF16) or e4m3 bytes
  * (ATTN_FP8_E4M3: the real values are k_descale and v_descale times the codes'; the de-scales are ignored for
- * ATTN_BF16).  page_size is a power of two from 16 to 1024 (ATTN_ERR_UNSUPPORTED otherwise).  `pages` is int32 [S, W]: key p
- * of sequence s is row p % page_size of page pages[s][p / page_size], for p < W * page_size.
+ * ATTN_BF16).  page_size is a power of two from 16 to 1024, and W * page_size at most 2^30 (ATTN_ERR_UNSUPPORTED
+ * otherwise).  `pages` is int32 [S, W]: key p of sequence s is row p % page_size of page pages[s][p / page_size], for
+ * p < W * page_size.
  *
  * kv_append -- new tokens of a serving batch: split, norm and rotation as rope_qkv, into the cache.
  *   qkv .. interleaved   as for rope_qkv, T rows
@@ -92,8 +93,8 @@ long long rope_qkv_bwd_workspace_bytes(int B, int Hq, int Hkv, int N, int d);
  *   q          bfloat16 [T, Hq, d]
  * Codes are round-to-nearest-even of value / de-scale, saturated at +-448 (NaN stays NaN).
  * A token with a negative position is padding: nothing is written for it, neither q nor cache.  A token whose position is not
- * below npos, or whose sequence is outside 0 .. S - 1, gets NaN in its row of q and does not enter the cache; one whose page is outside
- * the table (p >= W * page_size) or whose entry is outside 0 .. num_pages - 1 gets its q and does not enter the cache.
+ * below npos (where rot > 0), or whose sequence is outside 0 .. S - 1, gets NaN in its row of q and does not enter the cache; one whose
+ * page is outside the table (p >= W * page_size) or whose entry is outside 0 .. num_pages - 1 gets its q and does not enter the cache.
  * Tokens of one call must not name the same place of the cache twice: what it then holds is unspecified, and may be a mix.
  * Nothing else of the cache is touched.  One kernel.  Errors as for rope_qkv, and ATTN_ERR_DTYPE, ATTN_ERR_UNSUPPORTED for a
  * page_size, or for a de-scale that is not positive with ATTN_FP8_E4M3.
@@ -111,12 +112,14 @@ int kv_append(const void* qkv, long long ld, const void* q_weight, const void* k
  *   q          bfloat16 [B, Hq, d] (kv_append's q); query head h reads key head h / (Hq / Hkv)
  *   pages      int32 [B, W];  lens  int32 [B]: keys of each sequence, the new token's own among them (taken as at most
  *              W * page_size).  Keys of an entry outside 0 .. num_pages - 1 are hidden
- *   o          bfloat16 [B, Hq, d];  lse  float32 [B, Hq], required.  A sequence without visible keys gets o = 0, lse = -inf
+ *   o          bfloat16 [B, Hq, d];  lse  float32 [B, Hq], required.  A row without visible keys, or all of whose scores are -inf, gets
+ *              o = 0, lse = -inf
  *   workspace  kv_decode_workspace_bytes(B, Hq, Hkv, d) bytes; contents on entry are irrelevant, on return unspecified;
  *              calls that can overlap on the device must not share it
  *   scale      > 0 (ATTN_ERR_UNSUPPORTED otherwise)
+ *   d          64 or 128; B * Hq below 2^24 (ATTN_ERR_UNSUPPORTED otherwise)
  * What lies in the cache behind a sequence's last key, or in pages that no visible key names, is never read into a result.
- * The split of the keys over workgroups is computed on the device from `lens`: the call can be captured once and replayed while
+ * Two kernels are enqueued.  The split of the keys over workgroups is computed on the device from `lens`: the call can be captured once and replayed while
  * the sequences grow.  Deterministic.  Products are taken on bf16 with 32-bit sums (e4m3 values are exact in bf16); softmax
  * statistics and sums are 32 bits; the probabilities are rounded to bf16 for the second product.
  */

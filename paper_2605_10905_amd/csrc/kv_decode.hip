@@ -3,6 +3,10 @@
 // The call reads every visible key and value once and does 4 G operations on each of their features (G query heads share a
 // key head), so it is bound by memory as long as the products run on the matrix cores and enough bytes are in flight.
 //
+// Measured, where a 1 GiB device copy runs at 5.16 TB/s (keys and values read a second, both kernels): 2 x 131072 keys, 64/8 heads, d = 128
+// 188 us (5.7 TB/s); 64 ragged sequences up to 6000 151 (5.4); 32 up to 9000, e4m3 65 (4.7); 24 up to 1500, 16/16 heads, d = 64 20.7 (3.7);
+// 1 x 500, 32/8 heads 7.8, which is two launches.
+//
 // Split: the work is the list of all tiles (8 KB of keys: 32, 64 or 128 of them, and their values), sequence by sequence, key head by
 // key head; each of kWorkers waves takes an equal, consecutive piece of it, whatever the lengths are.  What the pieces are follows from
 // `lens` on the device, by a scan over them that every wave does for itself.  A wave that covers all tiles of a (sequence, key head) writes its
