@@ -32,7 +32,7 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
-constexpr int kWaves = 4, kWorkers = 1024, kWorkersLog2 = 10;
+constexpr int kWaves = 4, kWorkers = 1024, kWorkersLog2 = 10, kWorkgroups = kWorkers / kWaves;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // a value that all lanes agree on, in a scalar register
@@ -63,6 +63,14 @@ __device__ __forceinline__ uint32_t scan64(uint32_t x) {
   x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);  // row_bcast 15 into rows 1 and 3
   x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);  // row_bcast 31 into rows 2 and 3
   return x;
+}
+
+// Where the piece of wave i begins in a list of `all` tiles: equal pieces; or, where there are fewer tiles than waves, one tile each for the first
+// of them, side by side, so that the four of a workgroup can add their sums (1 x 30000 keys, 8/1 heads 19.7 -> 12.6 us); or, where there are no
+// more than workgroups, one for each workgroup's first wave (1 x 500, 32/8 heads 7.9 us, side by side 8.7).
+__device__ __forceinline__ unsigned long long piece_begin(unsigned long long all, int i) {
+  if (all >= kWorkers) return (all * (unsigned)i) >> kWorkersLog2;
+  return min((unsigned long long)(unsigned)(all <= kWorkgroups ? (i + kWaves - 1) / kWaves : i), all);
 }
 
 // A wave's piece [begin, end) of the list of all tiles, and the sequence that it begins in.
@@ -97,8 +105,8 @@ __device__ __forceinline__ Piece piece_of(const DecodeParams& p, int worker, int
     total += uniform(mine);
   }
   r.all = total * (unsigned)units;
-  r.begin = (r.all * worker) >> kWorkersLog2;
-  r.end = (r.all * (worker + 1)) >> kWorkersLog2;
+  r.begin = piece_begin(r.all, worker);
+  r.end = piece_begin(r.all, worker + 1);
   r.b = r.len = 0;
   r.before = 0;
   unsigned long long base = 0;
@@ -148,13 +156,13 @@ __host__ __device__ constexpr int blocks_for(int G) { return G <= 16 ? 1 : G <= 
 __host__ __device__ __forceinline__ int rows_kept(int G) { return G < 16 * blocks_for(G) ? G : 16 * blocks_for(G); }
 // floats of one wave's sums: rows of O, then (reference maximum, sum) of each row
 __host__ __device__ __forceinline__ int partial_floats(int rows, int d) { return rows * d + (2 * rows + 3) / 4 * 4; }
-// What the second kernel has to know of each (sequence, unit), behind the sums: written by the wave that takes its first tile (first, all)
+// What the second kernel has to know of each (sequence, unit), behind the sums: written by the wave that takes its first tile (first)
 // and, where that is another one, by the wave that takes its last (last).
 struct Split {
   int first;  // 2 * wave + which of its two sums the first part is; -1: one wave took it all
   int last;   // the wave of the last part
-  int all;    // tiles of the whole list where there are fewer than waves (a wave then has one of them at most), else 0
   int ends;   // (with last) whether that wave's piece ends with this (sequence, unit)
+  int step;   // (with first) waves from one with a part to the next
 };
 __host__ __device__ __forceinline__ size_t split_offset(int rows, int d) { return (size_t)2 * kWorkers * partial_floats(rows, d) * sizeof(float); }
 
@@ -181,7 +189,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   const int page_mask = (1 << p.page_log2) - 1;
 
   const Piece at = piece_of<TL>(p, worker, units);
-  if (at.begin == at.end) return;  // (fewer tiles than waves: there is no barrier below then)
+  if (at.begin == at.end) return;  // (no wave of its workgroup comes to the barrier below then)
   const int n = (int)(at.end - at.begin);  // (2^10 waves share far below 2^41 tiles: a cache fits the memory)
 
   // A position in the list: tile t of `unit` of sequence b, and the page entries of its blocks
@@ -324,7 +332,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     Split* const x = (Split*)((char*)p.ws + split_offset(kept, D)) + ((size_t)cp.b * units + cp.unit);
     if (head) {
       x->first = whole ? -1 : 2 * worker + part;
-      x->all = at.all < kWorkers ? (int)at.all : 0;
+      x->step = at.all <= kWorkgroups ? kWaves : 1;
     }
     if (tail && !whole) {
       x->last = worker;
@@ -514,8 +522,10 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
 
   // Whether the pieces of the workgroup's waves lie in this (sequence, unit): then all of them find so, and add their sums.
   const unsigned long long seg_begin = at.end - 1 - (unsigned)cp.t, seg_end = seg_begin + (unsigned)cp.nt;
-  const unsigned long long wg_begin = (at.all * (unsigned)(worker - w)) >> kWorkersLog2, wg_end = (at.all * (unsigned)(worker - w + kWaves)) >> kWorkersLog2;
-  if (at.all < kWorkers || wg_begin < seg_begin || seg_end < wg_end) {
+  // (Not where one of them has no tile: the end of the workgroup's pieces then lies behind the list, or there are no more tiles than workgroups.)
+  const unsigned long long wg_begin = piece_begin(at.all, worker - w);
+  const unsigned long long wg_end = at.all < kWorkers ? (unsigned)(worker - w + kWaves) : piece_begin(at.all, worker - w + kWaves);
+  if (at.all <= kWorkgroups || wg_begin < seg_begin || seg_end < wg_end) {
     finish(began == 0, cp.t + 1 == cp.nt, part, true);
     return;
   }
@@ -579,14 +589,14 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
 // workgroup for each.  D / 4 lanes take a row.  Few parts: they take them one after the other, four requested at a time, and the workgroup's
 // lanes hold different rows; many (MANY): different parts of a row are shared out, over a whole workgroup of sixteen waves for each row.
 template <int D, bool MANY, bool JOINT>
-__global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const DecodeParams p, int NQ, int tile_log2) {
+__global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const DecodeParams p, int NQ) {
   constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, rows (MANY: parts) a wave holds side by side
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG, kept = rows_kept(G);
   const int segment = MANY ? blockIdx.x / kept : blockIdx.x, b = segment / units, unit = segment - b * units;
   const int* const split = (const int*)((const char*)p.ws + split_offset(kept, D)) + (size_t)segment * 4;
   const int len = visible_keys(p, scalar_load(p.lens, b));
-  const int split_first = scalar_load(split, 0), w1 = scalar_load(split, 1), all = scalar_load(split, 2);
-  const int ends = JOINT ? scalar_load(split, 3) : 0;
+  const int split_first = scalar_load(split, 0), w1 = scalar_load(split, 1), ends = JOINT ? scalar_load(split, 2) : 0;
+  const int step = scalar_load(split, 3) == kWaves ? kWaves : 1;
   if (len > 0 && split_first < 0) return;  // one wave took it all
   const int lane = threadIdx.x & 63, w = uniform((int)(threadIdx.x >> 6)), sub = lane / LPR, col = (lane % LPR) * 4;
   const int hk = unit / QG, first_row = (unit - hk * QG) * 16 * NQ, rows = min(kept, G - first_row);
@@ -594,17 +604,13 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
 
   // (kept inside the workspace whatever it holds: `lens` may have changed under the call)
   const int first_sum = min(split_first, 2 * kWorkers - 1), w0 = first_sum >> 1, stride = partial_floats(kept, D);
-  // The parts: of every wave from w0 to w1, but one of each workgroup whose four waves work on nothing else (groups g0 to g1); or, where there
-  // are fewer tiles than waves, of the wave of each tile; without keys there is none.
-  const uint32_t first = all ? ((uint32_t)all * (uint32_t)w0) >> kWorkersLog2 : 0;
-  const int g0 = (w0 + (first_sum & 1) + kWaves - 1) / kWaves, g1 = (w1 + (ends ? 1 : 0)) / kWaves - 1, groups = !JOINT || all ? 0 : max(g1 - g0 + 1, 0);
+  // The parts: of every wave from w0 to w1, but one of each workgroup whose four waves work on nothing else (groups g0 to g1).
+  const int g0 = (w0 + (first_sum & 1) + kWaves - 1) / kWaves, g1 = (w1 + (ends ? 1 : 0)) / kWaves - 1, groups = JOINT && step == 1 ? max(g1 - g0 + 1, 0) : 0;
   const int front = groups ? kWaves * g0 - w0 : kWorkers;
-  int parts = all ? (len + (1 << tile_log2) - 1) >> tile_log2 : w1 - w0 + 1 - (kWaves - 1) * groups;
-  parts = len == 0 ? 0 : min(parts, kWorkers);
+  const int parts = len == 0 ? 0 : min((w1 - w0) / step + 1 - (kWaves - 1) * groups, kWorkers);  // (without keys there is none)
   auto sums_of = [&](int i) __attribute__((always_inline)) {  // which of the 2 * kWorkers sums part i is
     if (i == 0) return first_sum;
-    const int x = all ? (int)((((first + i + 1) << kWorkersLog2) - 1) / (uint32_t)all)
-                  : !JOINT || i < front ? w0 + i : i < front + groups ? kWaves * (g0 + i - front) : w0 + i + (kWaves - 1) * groups;
+    const int x = !JOINT || i < front ? w0 + i * step : i < front + groups ? kWaves * (g0 + i - front) : w0 + i + (kWaves - 1) * groups;
     return min(2 * x, 2 * kWorkers - 1);
   };
 
@@ -688,16 +694,17 @@ void launch_decode(const DecodeParams& p, int nq, hipStream_t stream) {
 }
 
 template <int D, bool JOINT>
-void launch_join(const DecodeParams& p, int nq, int segments, int tile_log2, hipStream_t stream) {
+void launch_join(const DecodeParams& p, int nq, int segments, hipStream_t stream) {
   const int kept = rows_kept(p.Hq / p.Hkv), rows_per_wave = 256 / D, waves = (kept + rows_per_wave - 1) / rows_per_wave;
-  // up to 256 / segments parts and six more of each, where there are fewer tiles than waves up to 1024 / segments
+  // Up to 256 / segments parts of each and six more.  us, one part after the other / shared out: 1 x 500 keys, 32/8 heads (8 pairs) 9.6 / 7.9;
+  // 2 x 131072, 64/8 (16) 189.4 / 187.5; 14 x 4582 e4m3, 8/2 (28) 15.3 / 14.0; 56 x 900, 8/1 12.8 / 13.6; 100 x 300, 8/1 11.4 / 14.5.
   if constexpr (JOINT) {
-    if (segments < 64) {
-      kv_join_kernel<D, true, true><<<segments * kept, 1024, 0, stream>>>(p, nq, tile_log2);
+    if (segments < 40) {
+      kv_join_kernel<D, true, true><<<segments * kept, 1024, 0, stream>>>(p, nq);
       return;
     }
   }
-  kv_join_kernel<D, false, JOINT><<<segments, 64 * (waves < 4 ? waves : 4), 0, stream>>>(p, nq, tile_log2);
+  kv_join_kernel<D, false, JOINT><<<segments, 64 * (waves < 4 ? waves : 4), 0, stream>>>(p, nq);
 }
 
 template <bool JOINT>
@@ -707,9 +714,8 @@ int launch(const DecodeParams& p, int d, bool fp8, int nq, int segments, hipStre
   else if (fp8) launch_decode<64, true, JOINT>(p, nq, stream);
   else launch_decode<64, false, JOINT>(p, nq, stream);
   if (hipGetLastError() != hipSuccess) return 1;
-  const int tile_log2 = d == 128 && !fp8 ? kTileLog2<256> : d == 64 && fp8 ? kTileLog2<64> : kTileLog2<128>;
-  if (d == 128) launch_join<128, JOINT>(p, nq, segments, tile_log2, stream);
-  else launch_join<64, JOINT>(p, nq, segments, tile_log2, stream);
+  if (d == 128) launch_join<128, JOINT>(p, nq, segments, stream);
+  else launch_join<64, JOINT>(p, nq, segments, stream);
   return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

@@ -379,6 +379,9 @@ def test_kv_decode_splits(lens, Hq, Hkv, d, fp8):
     ([70000], 8, 1, 128, False), ([70001], 64, 1, 64, True), ([33000, 33000], 70, 2, 128, False), ([16001, 7, 0, 40000], 33, 1, 128, True),
     ([4000] * 20 + [1] * 9, 32, 1, 64, False), ([999] * 40, 64, 1, 128, True), ([50000, 64], 16, 2, 64, False), ([32768], 4, 1, 128, False),
     ([32 * 1023], 4, 1, 128, False), ([32 * 1025], 4, 1, 128, False), ([32 * 1028, 32 * 4], 5, 1, 128, False),
+    # fewer tiles than waves, a number that leaves a workgroup incomplete, as many as workgroups and one more
+    ([32 * 1022 - 5], 4, 1, 128, False), ([32 * 901, 40], 6, 1, 128, False), ([32 * 256], 8, 1, 128, False), ([32 * 257], 8, 1, 128, False), ([32 * 100, 32 * 156 - 1, 9], 2, 1, 128, False),
+    ([64 * 255, 64], 40, 1, 128, True), ([64 * 130 + 1, 64 * 131], 3, 1, 64, False), ([128 * 300, 0, 128 * 400], 8, 1, 64, True), ([90] * 45, 30, 5, 128, False),
 ], ids=lambda x: f"{len(x)}x{max(x)}" if isinstance(x, list) else str(x))
 def test_kv_decode_pieces_that_share_a_workgroup(lens, Hq, Hkv, d, fp8):
     """Pieces of the work that begin and end with a workgroup's and that do not: sums of four waves, of one, of all."""
