@@ -266,6 +266,12 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       from[i] = has ? ((((size_t)ld.e[i] * p.Hkv + hk) << p.page_log2) + ((j0 + (j0 + 16 * i < ld.len ? 16 * i : 0)) & page_mask)) * ROWB : 0;
       ok |= has && j0 + 16 * i < ld.len ? 1u << i : 0u;
     }
+    // Pieces behind the last key read the tile's first rows once more, which are in the caches (1000 ragged sequences up to 60
+    // keys, 32/8 heads 55.8 -> 51.3 us; long ones are not slower).
+    auto at_piece = [&](int c) __attribute__((always_inline)) {
+      const size_t other = from[0] - (size_t)((c % LPB) * PIECE_ROWS * ROWB);
+      return c % LPB > 0 && j0 + c * PIECE_ROWS >= ld.len ? other : from[c / LPB];
+    };
     const uint32_t to = ring + slot * (2 * TILEB);
     if constexpr (QRING) {
       if (ld.t == 0 || ld_first) {
@@ -276,9 +282,9 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
       ld_first = false;
     }
 #pragma unroll
-    for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.k + from[c / LPB], koff[c % LPB], to + c * 1024);
+    for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.k + at_piece(c), koff[c % LPB], to + c * 1024);
 #pragma unroll
-    for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.v + from[c / LPB], voff[c % LPB], to + TILEB + c * 1024);
+    for (int c = 0; c < LPT; ++c) attn_lds_dma16((const char*)p.v + at_piece(c), voff[c % LPB], to + TILEB + c * 1024);
     return ok;
   };
 

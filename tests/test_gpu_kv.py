@@ -577,6 +577,38 @@ def test_kv_decode_many_pairs(G, d, fp8):
     ku.decode_check(o, lse, q, cache, d ** -0.5)
 
 
+def test_two_captured_graphs_share_a_workspace():
+    """Calls of other sizes, each in a graph of its own, over one workspace: replayed in turn on one stream, with eager work between."""
+    A = _A()
+    gen = ku.generator(99)
+    caches = [ku.Cache(gen, lens, Hkv, 128, 32, False) for lens, Hkv in (([5000, 30], 2), ([70] * 40, 8), ([1], 1))]
+    qs = [_q(gen, len(c.lens), 4 * c.k.shape[1], 128) for c in caches]
+    want = [_decode(q, c, 0.09) for q, c in zip(qs, caches)]
+    ws = torch.full((max(A.kv_decode_workspace_bytes(len(c.lens), q.shape[1], c.k.shape[1], 128) for q, c in zip(qs, caches)) // 4,), NAN, device="cuda")
+    outs, graphs = [(torch.empty_like(o), torch.empty_like(lse)) for o, lse in want], []
+    lens = [torch.tensor(c.lens, dtype=torch.int32, device="cuda") for c in caches]
+
+    def call(i, stream=None):
+        q, c, (o, lse) = qs[i], caches[i], outs[i]
+        A.kv_decode(q, c.k, c.v, c.pages, lens[i], o, lse, ws, len(c.lens), q.shape[1], c.k.shape[1], 128, c.width, 32, c.num, 0.09, A.ATTN_BF16, stream=stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(3):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            call(i, torch.cuda.current_stream())
+    for i in (0, 1, 0, 2, 1, 1, 0, 2):
+        for t in outs[i]:
+            t.fill_(7.0)
+        graphs[i].replay()
+        call((i + 1) % 3)
+        torch.cuda.synchronize()
+        for k in (i, (i + 1) % 3):
+            assert torch.equal(outs[k][0], want[k][0]) and torch.equal(outs[k][1], want[k][1]), (i, k)
+        ws.fill_(1e30)
+
+
 # ---- together ----------------------------------------------------------------------------------
 
 
