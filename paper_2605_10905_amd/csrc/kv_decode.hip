@@ -15,7 +15,7 @@
 // their sums in LDS first.
 //
 // A wave streams its tiles through a ring of its own in LDS (two of 16 KB: 128 KB of a CU's four waves, of which at least half is in
-// flight), by direct-to-LDS loads, so that no barrier is needed anywhere.  Page entries come through the scalar cache, whose counter is
+// flight), by direct-to-LDS loads, so that no barrier is needed while it does.  Page entries come through the scalar cache, whose counter is
 // not the tiles'.  A block of 16 rows lies in one page (pages hold 16 rows or more).
 //
 // Products are taken transposed, as in attn_fwd: S^T = K Q^T and O^T += V^T P^T on the 16x16x32 MFMA, the queries of the group as its
