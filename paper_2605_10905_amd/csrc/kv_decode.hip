@@ -591,14 +591,15 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
   }
 }
 
-// Joins what the waves left of a (sequence, unit) that more than one of them took, or writes the rows of a sequence without keys; one
-// workgroup for each.  D / 4 lanes take a row.  Few parts: they take them one after the other, four requested at a time, and the workgroup's
-// lanes hold different rows; many (MANY): different parts of a row are shared out, over a whole workgroup of sixteen waves for each row.
+// Joins what the waves left of a (sequence, unit) that more than one of them took, or writes the rows of a sequence without keys.  D / 4 lanes
+// take a row.  Few parts: they take them one after the other, four requested at a time, and the workgroup's lanes hold different rows; many
+// (MANY): different parts of a row are shared out, over a whole workgroup of sixteen waves for each row.  `shares` workgroups
+// take a pair.
 template <int D, bool MANY, bool JOINT>
-__global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const DecodeParams p, int NQ) {
+__global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const DecodeParams p, int NQ, int shares) {
   constexpr int LPR = D / 4, PER = 64 / LPR, AT_ONCE = 4;  // lanes of a row, rows (MANY: parts) a wave holds side by side
   const int G = p.Hq / p.Hkv, QG = (G + 16 * NQ - 1) / (16 * NQ), units = p.Hkv * QG, kept = rows_kept(G);
-  const int segment = MANY ? blockIdx.x / kept : blockIdx.x, b = segment / units, unit = segment - b * units;
+  const int segment = shares == 1 ? blockIdx.x : blockIdx.x / shares, b = segment / units, unit = segment - b * units;
   const int* const split = (const int*)((const char*)p.ws + split_offset(kept, D)) + (size_t)segment * 4;
   const int len = visible_keys(p, scalar_load(p.lens, b));
   const int split_first = scalar_load(split, 0), w1 = scalar_load(split, 1), ends = JOINT ? scalar_load(split, 2) : 0;
@@ -656,13 +657,13 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
   };
 
   if constexpr (!MANY) {
-    for (int r = w * PER + sub; r < rows; r += blockDim.x / LPR) {
-      add_parts(r, 0, 1, AT_ONCE);
-      write(r);
-    }
+    const int r = (blockIdx.x - segment * shares) * (blockDim.x / LPR) + w * PER + sub;
+    if (r >= rows) return;
+    add_parts(r, 0, 1, AT_ONCE);
+    write(r);
   } else {
     __shared__ float so[16][D], sm[16], sl[16];
-    const int r = blockIdx.x - segment * kept;
+    const int r = blockIdx.x - segment * shares;
     if (r >= rows) return;
     add_parts(r, w * PER * AT_ONCE + sub, PER, 16 * PER * AT_ONCE);
 #pragma unroll
@@ -686,7 +687,7 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) kv_join_kernel(const Decode
 }
 
 // Workgroups add their sums where there are few enough (sequence, unit) pairs, on average two workgroups or more to each.  us, apart / added:
-// 64 x 4000 keys, 64/1 heads 61.2 / 44.8, 32/1 41.2 / 32.9; 128 x 4000, 32/2 heads 100 / 95; 1 x 131072 e4m3, 8/1 heads 23.1 / 17.3; 2 x 131072,
+// 64 x 4000 keys, 64/1 heads 61.2 / 44.8 (42.5 with the join's rows over more workgroups), 32/1 41.2 / 32.9; 128 x 4000, 32/2 heads 100 / 95; 1 x 131072 e4m3, 8/1 heads 23.1 / 17.3; 2 x 131072,
 // 64/8 heads 191.9 / 190.2.  Where it is seldom possible the code for it costs: 211 ragged sequences up to 140 keys, 32/4 heads 17.5 / 18.2;
 // 71 up to 1894, e4m3, 56/8 heads 23.8 / 24.3.
 bool sums_are_added(long long segments) { return segments <= 128; }
@@ -706,11 +707,12 @@ void launch_join(const DecodeParams& p, int nq, int segments, hipStream_t stream
   // 2 x 131072, 64/8 (16) 189.4 / 187.5; 14 x 4582 e4m3, 8/2 (28) 15.3 / 14.0; 56 x 900, 8/1 12.8 / 13.6; 100 x 300, 8/1 11.4 / 14.5.
   if constexpr (JOINT) {
     if (segments < 40) {
-      kv_join_kernel<D, true, true><<<segments * kept, 1024, 0, stream>>>(p, nq);
+      kv_join_kernel<D, true, true><<<segments * kept, 1024, 0, stream>>>(p, nq, kept);
       return;
     }
   }
-  kv_join_kernel<D, false, JOINT><<<segments, 64 * (waves < 4 ? waves : 4), 0, stream>>>(p, nq);
+  const int used = waves < 4 ? waves : 4, shares = (kept + used * rows_per_wave - 1) / (used * rows_per_wave);
+  kv_join_kernel<D, false, JOINT><<<segments * shares, 64 * used, 0, stream>>>(p, nq, shares);
 }
 
 template <bool JOINT>
