@@ -50,7 +50,7 @@ extern "C" {
  *   d          64 or 128 (ATTN_ERR_UNSUPPORTED otherwise)
  * Errors: ATTN_ERR_NULL (a missing pointer, or one weight without the other), ATTN_ERR_SHAPE (non-positive size,
  * Hq % Hkv != 0, ld too small or no multiple of 8, rot outside 0 .. d, N > npos without pos, misaligned pointer),
- * ATTN_ERR_UNSUPPORTED (d; rot no multiple of 16; eps negative or NaN; B * N * (Hq + 2 Hkv) of 2^31 or more), ATTN_ERR_LAUNCH.
+ * ATTN_ERR_UNSUPPORTED (d; rot no multiple of 16; eps negative or NaN; B * N * (Hq + 2 Hkv) above 2^31 - 1024), ATTN_ERR_LAUNCH.
  */
 int rope_qkv(const void* qkv, long long ld, const void* q_weight, const void* k_weight, float eps,
              const float* table, int npos, int rot, int interleaved, const int* pos,

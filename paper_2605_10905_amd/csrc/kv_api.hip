@@ -21,7 +21,7 @@ int check_rows(const void* qkv, bool need_qkv, long long ld, const void* wq, con
   if (misaligned(qkv, 16) || misaligned(wq, 16) || misaligned(wk, 16) || misaligned(table, 16)) return ATTN_ERR_SHAPE;
   if ((d != 64 && d != 128) || rot % 16 != 0) return ATTN_ERR_UNSUPPORTED;
   if (wq && !(eps >= 0.0f)) return ATTN_ERR_UNSUPPORTED;
-  if (((long long)Hq + 2ll * Hkv) > 0x7fffffffll || T > 0x7fffffffll / ((long long)Hq + 2ll * Hkv)) return ATTN_ERR_UNSUPPORTED;
+  if (T > (0x7fffffffll - 1023) / ((long long)Hq + 2ll * Hkv)) return ATTN_ERR_UNSUPPORTED;  // rows are counted in 32 bits, a task past the last
   return ATTN_OK;
 }
 

@@ -8,7 +8,7 @@
 // rotated is dealt to the remaining lanes the same way.  The mean of squares is a sum over d / 16 neighbouring lanes (quad
 // permutations and a half-row mirror, no LDS).
 //
-// Measured, where a 1 GiB device copy runs at 5.16 TB/s: rope_qkv of 16384 tokens, 64/8 heads, d = 128 128 us (5.2 - 5.3 TB/s); kv_append of
+// Measured, where a 1 GiB device copy runs at 5.16 TB/s: rope_qkv of 16384 tokens, 64/8 heads, d = 128 128 - 131 us (5.1 - 5.3 TB/s); kv_append of
 // 9951 tokens, 32/8 heads into an e4m3 cache 45 us (5.0); rope_qkv_bwd of 8192 tokens, 16/16 heads 54 us (5.0) and 5 for the sums of the
 // weights' gradients; one token 3.9 - 4.6, which is a launch.
 #include "attn_device.h"
@@ -22,10 +22,11 @@ constexpr int kMostWorkgroups = 1 << 20;  // (a launch holds 2^32 threads)
 constexpr int kMostPartials = 1024;  // workgroups of a backward pass, each with its sums of the weights' gradients
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-// A wave takes kSpan groups of heads of a token, unless all groups can be taken by one wave each that start at once (4 waves on each of 1024
-// SIMDs): the smallest calls last as long as one wave's chain.  us at span 1 / 3 / 4 / 5 / 8: 16384 tokens of 64/8 heads, d = 128
-// 157 / 131 / 128 / 127 / 130; 9951 tokens of 32/8 heads into an e4m3 cache 57.6 / 45.3 / 45.0 / 46.2 / 47.9.
-constexpr int kSpan = 4, kFewTasks = 4096;
+// A wave takes kRowSpan (kv_append: kGroupSpan) steps, unless all steps can be taken by one wave each that start at once (4 waves on each of 1024
+// SIMDs): the smallest calls last as long as one wave's chain (64 tokens of 64/8 heads appended by spans of 4 5.8 us, of 1 4.8).  us at span
+// 1 / 3 / 4 / 6 / 8: rope_qkv of 16384 tokens of 64/8 heads, d = 128 157 / 130 / 128 / 132 / 131, of 30000 of 8/1 - / 40.6 / 41.0 / 42.6 / 47.3, of
+// 1000 of 32/8 7.7 / 6.9 / 7.3 / 8.0 / 9.4; 9951 tokens of 32/8 heads into an e4m3 cache 57.6 / 45.3 / 45.0 / - / 47.9.
+constexpr int kRowSpan = 3, kGroupSpan = 4, kFewTasks = 4096;
 
 // sum over the LPR (4 or 8) neighbouring lanes of a row, the same value in all of them
 template <int LPR>
@@ -82,25 +83,26 @@ __device__ __forceinline__ void load_angles(const RopeParams& p, const Chunks& c
   }
 }
 
-// the rotation (SIGN 1) or its transpose (-1)
+// The rotation (SIGN 1) or its transpose (-1).  Here and in the norm the fused products are written out, so that rope_qkv and kv_append give
+// the same bits.
 template <int SIGN>
 __device__ __forceinline__ void rotate(bool interleaved, float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) {
   if (!interleaved) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float s = SIGN * sn[i], x = a[i], y = b[i];
-      a[i] = x * cs[i] - y * s;
-      b[i] = y * cs[i] + x * s;
+      a[i] = fmaf(x, cs[i], -(y * s));
+      b[i] = fmaf(y, cs[i], x * s);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float s = SIGN * sn[i], x = a[2 * i], y = a[2 * i + 1];
-      a[2 * i] = x * cs[i] - y * s;
-      a[2 * i + 1] = y * cs[i] + x * s;
+      a[2 * i] = fmaf(x, cs[i], -(y * s));
+      a[2 * i + 1] = fmaf(y, cs[i], x * s);
       const float s2 = SIGN * sn[4 + i], x2 = b[2 * i], y2 = b[2 * i + 1];
-      b[2 * i] = x2 * cs[4 + i] - y2 * s2;
-      b[2 * i + 1] = y2 * cs[4 + i] + x2 * s2;
+      b[2 * i] = fmaf(x2, cs[4 + i], -(y2 * s2));
+      b[2 * i + 1] = fmaf(y2, cs[4 + i], x2 * s2);
     }
   }
 }
@@ -109,9 +111,9 @@ template <int LPR>
 __device__ __forceinline__ float inverse_rms(const float (&a)[8], const float (&b)[8], float eps) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s += a[i] * a[i] + b[i] * b[i];
+  for (int i = 0; i < 8; ++i) s = fmaf(a[i], a[i], fmaf(b[i], b[i], s));
   // 1 / sqrt, not the approximate reciprocal root: a row's error would be common to all of its features
-  return 1.f / sqrtf(row_sum<LPR>(s) * (1.f / (16 * LPR)) + eps);
+  return 1.f / sqrtf(fmaf(row_sum<LPR>(s), 1.f / (16 * LPR), eps));
 }
 
 // eight codes of x / descale, round to nearest even, saturated; NaN stays NaN
@@ -131,15 +133,115 @@ __device__ __forceinline__ u32x2 to_e4m3(const float (&x)[8], float descale) {
   return u32x2{(uint32_t)w[0], (uint32_t)w[1]};
 }
 
-enum { kLayout = 0, kCacheBf16 = 1, kCacheFp8 = 2 };
+// norm and rotation of a row of q or k; NaN where its position is not in the table
+template <int LPR>
+__device__ __forceinline__ void turn_row(const RopeParams& p, float (&a)[8], float (&b)[8], const u32x4 (&weight)[2], const float (&cs)[8], const float (&sn)[8], bool good) {
+  if (p.wq) {
+    float wa[8], wb[8];
+    unpack(weight[0], wa);
+    unpack(weight[1], wb);
+    const float r = inverse_rms<LPR>(a, b, p.eps);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      a[i] = a[i] * r * wa[i];
+      b[i] = b[i] * r * wb[i];
+    }
+  }
+  rotate<1>(p.interleaved, a, b, cs, sn);
+  if (!good) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
+  }
+}
+__device__ __forceinline__ void load_weights(const RopeParams& p, const Chunks& c, u32x4 (&wq)[2], u32x4 (&wk)[2]) {
+  if (!p.wq) return;
+  wq[0] = *(const u32x4*)((const char*)p.wq + c.a * 16);
+  wq[1] = *(const u32x4*)((const char*)p.wq + c.b * 16);
+  wk[0] = *(const u32x4*)((const char*)p.wk + c.a * 16);
+  wk[1] = *(const u32x4*)((const char*)p.wk + c.b * 16);
+}
 
+// A lane's row: head h of token t.  rope_qkv and its backward deal the rows of all tokens to the waves one after the other, 64 / (d / 16) at a
+// time, so that no lane idles whatever the number of heads is (a wave for each token / this, us: 30000 tokens of 8/1 heads 47.4 / 40.5, backward
+// 68.2 / 53.5; 32768 of 16/4, d = 64 51.9 / 47.2, backward 79 / 67; 16384 of 64/8 128.7 / 129.9).
+struct Place {
+  int t, h;
+};
+// (ONE: all rows that a wave holds at once are of one token, a multiple of them its heads; positions then come by scalar loads: backward of 16384
+// tokens of 32/8 heads 121 -> 117 us.)
+template <bool ONE>
+__device__ __forceinline__ Place place_of(int row, int H) {
+  Place x;
+  x.t = (ONE ? __builtin_amdgcn_readfirstlane(row) : row) / H;
+  x.h = row - x.t * H;
+  return x;
+}
 // scalar load of what no kernel writes while this one runs
 __device__ __forceinline__ int scalar_load(const int* p, size_t i) { return ((const __attribute__((address_space(4))) int*)p)[i]; }
 
-// One task, by one wave: `span` groups of 64 / (d / 16) consecutive heads of one token.  The token's position, page and angles and the norms'
-// weights are fetched once for all of them, the rows of the next group while the ones of this group are computed.
-template <int D, int MODE>
-__device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int span, int task) {
+// One task of rope_qkv, by one wave: `span` times 64 / (d / 16) consecutive rows.  A token's angles are fetched where a lane's row is the first of
+// it, the rows and positions one step ahead.
+template <int D>
+__device__ __forceinline__ void rope_task(const RopeParams& p, int rows, int span, int task) {
+  constexpr int LPR = D / 16, RPW = 64 / LPR;
+  const int lane = threadIdx.x & 63, H = p.Hq + 2 * p.Hkv;
+  const Chunks c = chunks_of<LPR>(lane % LPR, p.rot);
+  const int first = task * span * RPW + lane / LPR, steps = min(span, (rows - task * span * RPW + RPW - 1) / RPW);
+
+  u32x4 xa, xb, wq[2], wk[2];
+  int pos = 0;
+  auto fetch = [&](const Place& x, bool other) __attribute__((always_inline)) {  // (of another token; rows past the last re-read it)
+    const int t = min(x.t, p.T - 1), h = x.t < p.T ? x.h : H - 1;
+    if (other && p.pos) pos = p.pos[t];
+    const char* const src = (const char*)p.qkv + ((size_t)t * p.ld + (size_t)h * D) * 2;
+    xa = *(const u32x4*)(src + c.a * 16);
+    xb = *(const u32x4*)(src + c.b * 16);
+  };
+  Place next = place_of<false>(min(first, rows - 1), H);
+  if (first >= rows) next.t = p.T;
+  fetch(next, true);
+  load_weights(p, c, wq, wk);
+  const int whole = RPW / H, rest = RPW - whole * H;  // tokens and heads that RPW rows are
+
+  int have = -1, bb = 0, n = 0;  // the token that the following are of
+  bool good = false;
+  float cs[8], sn[8];
+  for (int g = 0; g < steps; ++g) {
+    const Place x = next;
+    const u32x4 ya = xa, yb = xb;
+    if (x.t != have) {
+      have = x.t;
+      bb = x.t / p.N;
+      n = x.t - bb * p.N;
+      const int at = p.pos ? pos : n;
+      good = p.rot == 0 || (unsigned)at < (unsigned)p.npos;
+      load_angles(p, c, good ? at : 0, cs, sn);
+    }
+    next.h += rest;
+    next.t += whole;
+    if (next.h >= H) {
+      next.h -= H;
+      ++next.t;
+    }
+    if (g + 1 < steps) fetch(next, next.t != x.t);
+    if (x.t >= p.T) continue;
+    const bool is_q = x.h < p.Hq, is_v = x.h >= p.Hq + p.Hkv;
+    float a[8], b[8];
+    unpack(ya, a);
+    unpack(yb, b);
+    if (!is_v) turn_row<LPR>(p, a, b, is_q ? wq : wk, cs, sn, good);
+    const int hk = is_q ? x.h : is_v ? x.h - p.Hq - p.Hkv : x.h - p.Hq, Hk = is_q ? p.Hq : p.Hkv;
+    char* const dst = (char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
+    *(u32x4*)(dst + c.a * 16) = is_v ? ya : pack(a);
+    *(u32x4*)(dst + c.b * 16) = is_v ? yb : pack(b);
+  }
+}
+
+// One task of kv_append, by one wave: `span` groups of 64 / (d / 16) consecutive heads of one token.  The token's position, page and angles and the
+// norms' weights are fetched once for all of them, the rows of the next group while the ones of this group are computed.  (Rows dealt as
+// rope_qkv's: 9951 tokens of 32/8 heads into an e4m3 cache 45.4 -> 47 - 49 us, 28/4 41 -> 43 - 47.)
+template <int D, bool FP8>
+__device__ __forceinline__ void append_task(const RopeParams& p, int groups, int span, int task) {
   constexpr int LPR = D / 16, RPW = 64 / LPR;
   const int lane = threadIdx.x & 63, j = lane % LPR, H = p.Hq + 2 * p.Hkv;
   const int spans = (groups + span - 1) / span, t = task / spans, g0 = (task - t * spans) * span, g1 = min(g0 + span, groups);
@@ -153,24 +255,15 @@ __device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int s
   };
   u32x4 xa, xb, wq[2], wk[2];
   fetch(g0, xa, xb);
-  if (p.wq) {
-    wq[0] = *(const u32x4*)((const char*)p.wq + c.a * 16);
-    wq[1] = *(const u32x4*)((const char*)p.wq + c.b * 16);
-    wk[0] = *(const u32x4*)((const char*)p.wk + c.a * 16);
-    wk[1] = *(const u32x4*)((const char*)p.wk + c.b * 16);
-  }
+  load_weights(p, c, wq, wk);
 
-  const int bb = MODE == kLayout ? t / p.N : 0, n = MODE == kLayout ? t - bb * p.N : 0;
-  const int pos = p.pos ? scalar_load(p.pos, t) : n;
+  const int pos = scalar_load(p.pos, t);
+  if (pos < 0) return;  // padding
+  const int seq = p.seq ? scalar_load(p.seq, t) : t;
+  const bool good = (p.rot == 0 || pos < p.npos) && (unsigned)seq < (unsigned)p.S;
   int entry = -1;
-  bool good = p.rot == 0 || (unsigned)pos < (unsigned)p.npos;
-  if constexpr (MODE != kLayout) {
-    if (pos < 0) return;  // padding
-    const int seq = p.seq ? scalar_load(p.seq, t) : t;
-    good = good && (unsigned)seq < (unsigned)p.S;
-    if (good && (pos >> p.page_log2) < p.W) entry = scalar_load(p.pages, (size_t)seq * p.W + (pos >> p.page_log2));
-    if ((unsigned)entry >= (unsigned)p.num_pages) entry = -1;
-  }
+  if (good && (pos >> p.page_log2) < p.W) entry = scalar_load(p.pages, (size_t)seq * p.W + (pos >> p.page_log2));
+  if ((unsigned)entry >= (unsigned)p.num_pages) entry = -1;
   float cs[8], sn[8];
   load_angles(p, c, good ? pos : 0, cs, sn);
 
@@ -183,36 +276,14 @@ __device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int s
     float a[8], b[8];
     unpack(ya, a);
     unpack(yb, b);
-    if (!is_v) {
-      if (p.wq) {
-        float wa[8], wb[8];
-        unpack(is_q ? wq[0] : wk[0], wa);
-        unpack(is_q ? wq[1] : wk[1], wb);
-        const float r = inverse_rms<LPR>(a, b, p.eps);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          a[i] = a[i] * r * wa[i];
-          b[i] = b[i] * r * wb[i];
-        }
-      }
-      rotate<1>(p.interleaved, a, b, cs, sn);
-      if (!good) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
-      }
-    }
-    const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq;
-    char* dst;
-    if constexpr (MODE == kLayout) {
-      const int Hk = is_q ? p.Hq : p.Hkv;
-      dst = (char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
-    } else if (is_q) {
-      dst = (char*)p.q + ((size_t)t * p.Hq + hk) * (D * 2);
-    } else {
+    if (!is_v) turn_row<LPR>(p, a, b, is_q ? wq : wk, cs, sn, good);
+    char* dst = (char*)p.q + ((size_t)t * p.Hq + h) * (D * 2);
+    if (!is_q) {
       if (!good || entry < 0) continue;
+      const int hk = is_v ? h - p.Hq - p.Hkv : h - p.Hq;
       const size_t place = (((size_t)entry * p.Hkv + hk) << p.page_log2) + (pos & ((1 << p.page_log2) - 1));
-      dst = (char*)(is_v ? p.v : p.k) + place * (D * (MODE == kCacheFp8 ? 1 : 2));
-      if constexpr (MODE == kCacheFp8) {
+      dst = (char*)(is_v ? p.v : p.k) + place * (D * (FP8 ? 1 : 2));
+      if constexpr (FP8) {
         const float descale = is_v ? p.v_descale : p.k_descale;
         *(u32x2*)(dst + c.a * 8) = to_e4m3(a, descale);
         *(u32x2*)(dst + c.b * 8) = to_e4m3(b, descale);
@@ -224,16 +295,22 @@ __device__ __forceinline__ void rope_task(const RopeParams& p, int groups, int s
   }
 }
 
-template <int D, int MODE>
-__global__ void __launch_bounds__(kWaves * 64) rope_qkv_kernel(const RopeParams p, int groups, int span, int tasks) {
+template <int D>
+__global__ void __launch_bounds__(kWaves * 64) rope_qkv_kernel(const RopeParams p, int rows, int span, int tasks) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) rope_task<D, MODE>(p, groups, span, task);
+  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) rope_task<D>(p, rows, span, task);
 }
 
-// The gradients.  A workgroup walks tasks (a token's 64 / (d / 16) heads) a grid apart and keeps what its lanes add to the
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kWaves * 64) kv_append_kernel(const RopeParams p, int groups, int span, int tasks) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) append_task<D, FP8>(p, groups, span, task);
+}
+
+// The gradients.  A workgroup walks tasks (64 / (d / 16) consecutive rows) a grid apart and keeps what its lanes add to the
 // weights' gradients in registers; the sums over lanes, waves and workgroups follow in a fixed order.
-template <int D, bool NORM>
-__global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopeParams p, int groups, int tasks) {
+template <int D, bool NORM, bool ONE>
+__global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopeParams p, int rows, int tasks) {
   constexpr int LPR = D / 16, RPW = 64 / LPR;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int j = lane % LPR, H = p.Hq + 2 * p.Hkv;
@@ -243,8 +320,10 @@ __global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopePar
   for (int i = 0; i < 8; ++i) acc[0][0][i] = acc[0][1][i] = acc[1][0][i] = acc[1][1][i] = 0.f;
 
   for (int task = blockIdx.x * kWaves + w; task < tasks; task += gridDim.x * kWaves) {
-    const int t = task / groups, h = (task % groups) * RPW + lane / LPR;
-    if (h >= H) continue;
+    const int row = task * RPW + lane / LPR;
+    if (row >= rows) continue;
+    const Place x = place_of<ONE>(row, H);
+    const int t = x.t, h = x.h;
     const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.Hkv;
     const int hk = is_q ? h : is_v ? h - p.Hq - p.Hkv : h - p.Hq, Hk = is_q ? p.Hq : p.Hkv;
     const int n = t % p.N, bb = t / p.N;
@@ -256,7 +335,7 @@ __global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopePar
       *(u32x4*)(dst + c.b * 16) = gb4;
       continue;
     }
-    const int pos = p.pos ? p.pos[t] : n;
+    const int pos = !p.pos ? n : ONE ? scalar_load(p.pos, t) : p.pos[t];
     const bool good = p.rot == 0 || (unsigned)pos < (unsigned)p.npos;
     float a[8], b[8], cs[8], sn[8];
     unpack(ga4, a);
@@ -359,47 +438,53 @@ __global__ void __launch_bounds__(1024) rope_weight_sum_kernel(const float* part
 
 int launched() { return hipGetLastError() == hipSuccess ? 0 : 1; }
 
-int tasks_of(const RopeParams& p, int d, int* groups) {
-  const int rows = 1024 / d;  // heads a wave takes at once
-  *groups = (p.Hq + 2 * p.Hkv + rows - 1) / rows;
-  return p.T * *groups;  // (at most T * heads, which fits)
+// Rows of all tokens (below 2^31), and the tasks of `span` times 64 / (d / 16) of them.
+int rows_of(const RopeParams& p) { return p.T * (p.Hq + 2 * p.Hkv); }
+int tasks_of(int rows, int d, int span) { return (int)(((long long)rows + span * (1024 / d) - 1) / (span * (1024 / d))); }
+
+}  // namespace
+
+int rope_qkv_launch(const RopeParams& p, int d, hipStream_t stream) {
+  const int rows = rows_of(p), span = tasks_of(rows, d, 1) <= kFewTasks ? 1 : kRowSpan, tasks = tasks_of(rows, d, span);
+  const int grid = min((tasks - 1) / kWaves + 1, kMostWorkgroups);
+  if (d == 128) rope_qkv_kernel<128><<<grid, kWaves * 64, 0, stream>>>(p, rows, span, tasks);
+  else rope_qkv_kernel<64><<<grid, kWaves * 64, 0, stream>>>(p, rows, span, tasks);
+  return launched();
 }
 
-template <int MODE>
-int launch_rows(const RopeParams& p, int d, hipStream_t stream) {
-  int groups;
-  const int all = tasks_of(p, d, &groups), span = all <= kFewTasks ? 1 : kSpan;
+int kv_append_launch(const RopeParams& p, int d, bool fp8, hipStream_t stream) {
+  const int groups = tasks_of(p.Hq + 2 * p.Hkv, d, 1), span = (long long)p.T * groups <= kFewTasks ? 1 : kGroupSpan;
   const int tasks = p.T * ((groups + span - 1) / span), grid = min((tasks - 1) / kWaves + 1, kMostWorkgroups);
-  if (d == 128) rope_qkv_kernel<128, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
-  else rope_qkv_kernel<64, MODE><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
+  if (d == 128 && fp8) kv_append_kernel<128, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
+  else if (d == 128) kv_append_kernel<128, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
+  else if (fp8) kv_append_kernel<64, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
+  else kv_append_kernel<64, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, span, tasks);
+  return launched();
+}
+
+int rope_qkv_bwd_workgroups(long long T, long long heads, int d) {
+  const long long per = d >= 1024 ? 1 : 1024 / d, tasks = (T * heads + per - 1) / per, wgs = (tasks + kWaves - 1) / kWaves;
+  return (int)(wgs < kMostPartials ? wgs : kMostPartials);
+}
+
+namespace {
+
+template <int D, bool ONE>
+int launch_bwd(const RopeParams& p, hipStream_t stream) {
+  const int rows = rows_of(p), tasks = tasks_of(rows, D, 1), grid = rope_qkv_bwd_workgroups(p.T, p.Hq + 2 * p.Hkv, D);
+  if (!p.wq) {
+    rope_qkv_bwd_kernel<D, false, ONE><<<grid, kWaves * 64, 0, stream>>>(p, rows, tasks);
+    return launched();
+  }
+  rope_qkv_bwd_kernel<D, true, ONE><<<grid, kWaves * 64, 0, stream>>>(p, rows, tasks);
+  if (launched() != 0) return 1;
+  rope_weight_sum_kernel<D><<<2 * D / 16, 1024, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
   return launched();
 }
 
 }  // namespace
 
-int rope_qkv_launch(const RopeParams& p, int d, hipStream_t stream) { return launch_rows<kLayout>(p, d, stream); }
-
-int kv_append_launch(const RopeParams& p, int d, bool fp8, hipStream_t stream) {
-  return fp8 ? launch_rows<kCacheFp8>(p, d, stream) : launch_rows<kCacheBf16>(p, d, stream);
-}
-
-int rope_qkv_bwd_workgroups(long long T, long long heads, int d) {
-  const long long rows = d >= 1024 ? 1 : 1024 / d, tasks = T * ((heads + rows - 1) / rows), wgs = (tasks + kWaves - 1) / kWaves;
-  return (int)(wgs < kMostPartials ? wgs : kMostPartials);
-}
-
 int rope_qkv_bwd_launch(const RopeParams& p, int d, hipStream_t stream) {
-  int groups;
-  const int tasks = tasks_of(p, d, &groups), grid = rope_qkv_bwd_workgroups(p.T, p.Hq + 2 * p.Hkv, d);
-  if (p.wq) {
-    if (d == 128) rope_qkv_bwd_kernel<128, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
-    else rope_qkv_bwd_kernel<64, true><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
-    if (launched() != 0) return 1;
-    if (d == 128) rope_weight_sum_kernel<128><<<2 * 128 / 16, 1024, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
-    else rope_weight_sum_kernel<64><<<2 * 64 / 16, 1024, 0, stream>>>(p.partial, grid, p.dwq, p.dwk);
-  } else {
-    if (d == 128) rope_qkv_bwd_kernel<128, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
-    else rope_qkv_bwd_kernel<64, false><<<grid, kWaves * 64, 0, stream>>>(p, groups, tasks);
-  }
-  return launched();
+  if ((p.Hq + 2 * p.Hkv) % (1024 / d) == 0) return d == 128 ? launch_bwd<128, true>(p, stream) : launch_bwd<64, true>(p, stream);
+  return d == 128 ? launch_bwd<128, false>(p, stream) : launch_bwd<64, false>(p, stream);
 }

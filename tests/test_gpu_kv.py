@@ -27,6 +27,8 @@ ROPE = [
     (2, 5, 3, 1, 128, True, 128, False, True, 8), (2, 37, 6, 2, 64, True, 32, True, True, 0), (1, 33, 32, 8, 128, True, 64, True, False, 24),
     (3, 17, 7, 7, 64, False, 48, False, True, 0), (1, 130, 5, 5, 128, True, 16, False, False, 0), (2, 9, 16, 4, 128, False, 96, True, True, 8),
     (1, 300, 2, 1, 64, True, 16, True, False, 0), (4, 3, 12, 12, 128, True, 112, False, True, 0), (1, 7, 9, 3, 64, True, 0, False, True, 16),
+    # rows of a wave's step from one token, from two, from many; steps that end behind the last row
+    (5, 1000, 1, 1, 128, True, 128, False, True, 0), (1, 3001, 5, 1, 64, True, 64, False, False, 0), (2, 1500, 6, 1, 128, True, 64, True, True, 8), (3, 700, 12, 2, 64, False, 64, False, True, 0),
 ]
 
 
@@ -34,7 +36,7 @@ def _rope_inputs(case, seed):
     B, N, Hq, Hkv, d, norm, rot, inter, given, gap = case
     gen = ku.generator(seed)
     T, width = B * N, (Hq + 2 * Hkv) * d
-    npos = 400
+    npos = max(400, N)
     pos = torch.randint(0, npos, (T,), generator=gen, device="cuda", dtype=torch.int32) if given else None
     at = pos.cpu().tolist() if given else list(range(N)) * B
     tab = ku.table(npos, rot) if rot else None

@@ -74,7 +74,7 @@ def test_rows_are_checked(A, call):
     for kw in ({size: 0}, {size: -3}, dict(Hq=3, Hkv=2), dict(Hkv=0), dict(ld=4 * 64 - 8), dict(ld=4 * 64 + 4), dict(rot=-16), dict(rot=80), dict(npos=0), dict(qkv=P + 8),
                dict(table=P + 4), dict(k_weight=P + 2), dict(pos=P + 2), dict(d=0)):
         assert call(A, **kw) == 2, kw
-    for kw in (dict(d=32, rot=32), dict(d=96, ld=4 * 96), dict(d=256, ld=4 * 256), dict(rot=24), dict(eps=-1.0), dict(eps=float("nan")), {size: 2 ** 30}):
+    for kw in (dict(d=32, rot=32), dict(d=96, ld=4 * 96), dict(d=256, ld=4 * 256), dict(rot=24), dict(eps=-1.0), dict(eps=float("nan")), {size: 2 ** 30}, {size: (2 ** 31 - 1024) // 4 + 1}):
         assert call(A, **kw) == 4, kw
 
 
@@ -190,9 +190,10 @@ def _all_calls():
         for norm in (False, True):
             w = P if norm else None
             rope = dict(ROPE, q_weight=w, k_weight=w, ld=16 * d)
-            size = dict(B=2, Hq=4, Hkv=2, N=5, d=d)
-            calls += [("rope_qkv", dict(rope, q=P, k=P, v=P, **size)),
-                      ("rope_qkv_bwd", dict(rope, dq=P, dk=P, dv=P, dqkv=P, dld=16 * d, dq_weight=w, dk_weight=w, workspace=w, **size))]
+            for Hq, Hkv in ((12, 2), (5, 1)):  # (16 heads are whole steps of a wave, 7 are not)
+                size = dict(B=2, Hq=Hq, Hkv=Hkv, N=5, d=d)
+                calls += [("rope_qkv", dict(rope, q=P, k=P, v=P, **size)),
+                          ("rope_qkv_bwd", dict(rope, dq=P, dk=P, dv=P, dqkv=P, dld=16 * d, dq_weight=w, dk_weight=w, workspace=w, **size))]
             calls += [("kv_append", dict(rope, seq=P, pages=P, q=P, k_cache=P, v_cache=P, T=4, S=4, Hq=2, Hkv=1, d=d, W=2, page_size=16, num_pages=9, dtype=t)) for t in (0, 1)]
         # few and many (sequence, key head) pairs: 2, 100 and 200 of them, more with many heads to one
         calls += [("kv_decode", dict(q=P, k_cache=P, v_cache=P, pages=P, lens=P, o=P, lse=P, workspace=P, B=B, Hq=G, Hkv=1, d=d, W=2, page_size=16, num_pages=9,
