@@ -63,13 +63,10 @@ __device__ __forceinline__ Chunks chunks_of(int j, int rot) {
   return c;
 }
 
-// cosine and sine of the lane's eight pairs at position `pos` (inside the table); 1 and 0 where nothing is rotated
+// cosine and sine of the lane's eight pairs at position `pos` (inside the table); zeros, which nobody uses, where nothing is rotated
 __device__ __forceinline__ void load_angles(const RopeParams& p, const Chunks& c, int pos, float (&cs)[8], float (&sn)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    cs[i] = 1.f;
-    sn[i] = 0.f;
-  }
+  for (int i = 0; i < 8; ++i) cs[i] = sn[i] = 0.f;
   if (!c.rotated) return;
   const f32x4* const row = (const f32x4*)(p.table + (size_t)pos * p.rot);
   const int at0 = p.interleaved ? 2 * c.a : 4 * c.a, at1 = p.interleaved ? 2 * c.b : 4 * c.a + 2;
@@ -83,26 +80,25 @@ __device__ __forceinline__ void load_angles(const RopeParams& p, const Chunks& c
   }
 }
 
-// The rotation (SIGN 1) or its transpose (-1).  Here and in the norm the fused products are written out, so that rope_qkv and kv_append give
-// the same bits.
+// The rotation (SIGN 1) or its transpose (-1) of a pair.  Pairs that are not rotated keep their features (by an angle of zero an infinity in one
+// would make the other, which only shares the lane with it, NaN).  Here and in the norm the fused products are written out, so that rope_qkv and
+// kv_append give the same bits.
 template <int SIGN>
-__device__ __forceinline__ void rotate(bool interleaved, float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) {
+__device__ __forceinline__ void turn(bool rotated, float& x, float& y, float cs, float sn) {
+  const float s = SIGN * sn, u = fmaf(x, cs, -(y * s)), w = fmaf(y, cs, x * s);
+  x = rotated ? u : x;
+  y = rotated ? w : y;
+}
+template <int SIGN>
+__device__ __forceinline__ void rotate(bool rotated, bool interleaved, float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) {
   if (!interleaved) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = SIGN * sn[i], x = a[i], y = b[i];
-      a[i] = fmaf(x, cs[i], -(y * s));
-      b[i] = fmaf(y, cs[i], x * s);
-    }
+    for (int i = 0; i < 8; ++i) turn<SIGN>(rotated, a[i], b[i], cs[i], sn[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float s = SIGN * sn[i], x = a[2 * i], y = a[2 * i + 1];
-      a[2 * i] = fmaf(x, cs[i], -(y * s));
-      a[2 * i + 1] = fmaf(y, cs[i], x * s);
-      const float s2 = SIGN * sn[4 + i], x2 = b[2 * i], y2 = b[2 * i + 1];
-      b[2 * i] = fmaf(x2, cs[4 + i], -(y2 * s2));
-      b[2 * i + 1] = fmaf(y2, cs[4 + i], x2 * s2);
+      turn<SIGN>(rotated, a[2 * i], a[2 * i + 1], cs[i], sn[i]);
+      turn<SIGN>(rotated, b[2 * i], b[2 * i + 1], cs[4 + i], sn[4 + i]);
     }
   }
 }
@@ -135,7 +131,7 @@ __device__ __forceinline__ u32x2 to_e4m3(const float (&x)[8], float descale) {
 
 // norm and rotation of a row of q or k; NaN where its position is not in the table
 template <int LPR>
-__device__ __forceinline__ void turn_row(const RopeParams& p, float (&a)[8], float (&b)[8], const u32x4 (&weight)[2], const float (&cs)[8], const float (&sn)[8], bool good) {
+__device__ __forceinline__ void turn_row(const RopeParams& p, const Chunks& c, float (&a)[8], float (&b)[8], const u32x4 (&weight)[2], const float (&cs)[8], const float (&sn)[8], bool good) {
   if (p.wq) {
     float wa[8], wb[8];
     unpack(weight[0], wa);
@@ -147,7 +143,7 @@ __device__ __forceinline__ void turn_row(const RopeParams& p, float (&a)[8], flo
       b[i] = b[i] * r * wb[i];
     }
   }
-  rotate<1>(p.interleaved, a, b, cs, sn);
+  rotate<1>(c.rotated, p.interleaved, a, b, cs, sn);
   if (!good) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");
@@ -229,7 +225,7 @@ __device__ __forceinline__ void rope_task(const RopeParams& p, int rows, int spa
     float a[8], b[8];
     unpack(ya, a);
     unpack(yb, b);
-    if (!is_v) turn_row<LPR>(p, a, b, is_q ? wq : wk, cs, sn, good);
+    if (!is_v) turn_row<LPR>(p, c, a, b, is_q ? wq : wk, cs, sn, good);
     const int hk = is_q ? x.h : is_v ? x.h - p.Hq - p.Hkv : x.h - p.Hq, Hk = is_q ? p.Hq : p.Hkv;
     char* const dst = (char*)(is_q ? p.q : is_v ? p.v : p.k) + (((size_t)bb * Hk + hk) * p.N + n) * (D * 2);
     *(u32x4*)(dst + c.a * 16) = is_v ? ya : pack(a);
@@ -276,7 +272,7 @@ __device__ __forceinline__ void append_task(const RopeParams& p, int groups, int
     float a[8], b[8];
     unpack(ya, a);
     unpack(yb, b);
-    if (!is_v) turn_row<LPR>(p, a, b, is_q ? wq : wk, cs, sn, good);
+    if (!is_v) turn_row<LPR>(p, c, a, b, is_q ? wq : wk, cs, sn, good);
     char* dst = (char*)p.q + ((size_t)t * p.Hq + h) * (D * 2);
     if (!is_q) {
       if (!good || entry < 0) continue;
@@ -341,7 +337,7 @@ __global__ void __launch_bounds__(kWaves * 64) rope_qkv_bwd_kernel(const RopePar
     unpack(ga4, a);
     unpack(gb4, b);
     load_angles(p, c, good ? pos : 0, cs, sn);
-    rotate<-1>(p.interleaved, a, b, cs, sn);
+    rotate<-1>(c.rotated, p.interleaved, a, b, cs, sn);
     if (!good) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = b[i] = __builtin_nanf("");

@@ -1,0 +1,119 @@
+"""The operators of include/kv.h on the GPU: what particular values become."""
+import pytest
+import torch
+
+from tests import kv_util as ku
+from tests.kv_util import NAN
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def _A():
+    import paper_2605_10905_amd as A
+
+    return A
+
+
+# ---- features past `rot` -----------------------------------------------------------------------
+
+UNROTATED = [(d, rot, inter) for d in (64, 128) for rot in (0, 16, d // 2, d - 16) for inter in (False, True)]
+
+
+def _marked(gen, shape, rot):
+    """Rows [.., d] whose features from `rot` on hold infinities, NaN, the largest numbers and both zeros in places of no order: (rows, their
+    clean form: zero there)."""
+    x = torch.randn(shape, generator=gen, device="cuda").bfloat16()
+    values = torch.tensor([INF, -INF, NAN, torch.finfo(torch.bfloat16).max, torch.finfo(torch.bfloat16).min, -0.0, 0.0, 1.0], device="cuda").bfloat16()
+    which = torch.randint(0, len(values), shape, generator=gen, device="cuda")
+    put = torch.rand(shape, generator=gen, device="cuda") < 0.2
+    put[..., :rot] = False
+    clean = torch.where(put, torch.zeros_like(x), x)
+    return torch.where(put, values[which], x), clean
+
+
+def _same(got, want):
+    """Bit for bit, one NaN as good as another."""
+    nan = got.isnan() & want.isnan()
+    return bool((nan | (got.view(torch.int16) == want.view(torch.int16))).all())
+
+
+@pytest.mark.parametrize("d,rot,inter", UNROTATED)
+def test_features_that_are_not_rotated_are_copied(d, rot, inter):
+    """Without a norm z = x from feature `rot` on, whatever x is (infinities, NaN, -0), and the rotated features do not see them."""
+    A = _A()
+    B, N, Hq, Hkv = 2, 21, 5, 1
+    gen = ku.generator(201 + rot)
+    T, H = B * N, Hq + 2 * Hkv
+    tab = ku.table(N, rot) if rot else None
+    x, clean = _marked(gen, (T, H, d), rot)
+    heads = ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, H))
+
+    def run(x):
+        outs = [torch.empty((B, hi - lo, N, d), dtype=torch.bfloat16, device="cuda") for lo, hi in heads]
+        A.rope_qkv(x, H * d, None, None, 0.0, tab, N, rot, inter, None, *outs, B, Hq, Hkv, N, d)
+        return torch.cat([o.transpose(1, 2).reshape(T, -1, d) for o in outs], 1)
+
+    got, base = run(x.view(T, -1)), run(clean.view(T, -1))
+    torch.cuda.synchronize()
+    assert _same(got[..., rot:], x[..., rot:])
+    assert _same(got[:, :Hq + Hkv, :rot], base[:, :Hq + Hkv, :rot]) and _same(got[:, Hq + Hkv:], x[:, Hq + Hkv:])
+
+
+@pytest.mark.parametrize("d,rot,inter", UNROTATED)
+def test_gradients_of_features_that_are_not_rotated_are_copied(d, rot, inter):
+    A = _A()
+    B, N, Hq, Hkv = 2, 21, 5, 1
+    gen = ku.generator(202 + rot)
+    T, H = B * N, Hq + 2 * Hkv
+    tab = ku.table(N, rot) if rot else None
+    x, clean = _marked(gen, (T, H, d), rot)
+    heads = ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, H))
+
+    def run(x):
+        grads = [x[:, lo:hi].reshape(B, N, hi - lo, d).transpose(1, 2).contiguous() for lo, hi in heads]
+        out = torch.empty((T, H * d), dtype=torch.bfloat16, device="cuda")
+        A.rope_qkv_bwd(*grads, None, H * d, None, None, 0.0, tab, N, rot, inter, None, out, H * d, None, None, None, B, Hq, Hkv, N, d)
+        return out.view(T, H, d)
+
+    got, base = run(x), run(clean)
+    torch.cuda.synchronize()
+    assert _same(got[..., rot:], x[..., rot:]) and _same(got[:, :Hq + Hkv, :rot], base[:, :Hq + Hkv, :rot])
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d,rot,inter", UNROTATED)
+def test_features_that_are_not_rotated_enter_the_cache_as_they_are(d, rot, inter, fp8):
+    """bf16 as they are; e4m3 saturated at 448 with the value's sign, NaN as NaN."""
+    A = _A()
+    Hq, Hkv, page = 4, 2, 16
+    lens = [20, 1, 33]
+    gen = ku.generator(203 + rot)
+    T, H = sum(lens), Hq + 2 * Hkv
+    tab = ku.table(64, rot) if rot else None
+    x, clean = _marked(gen, (T, H, d), rot)
+    pos = torch.tensor([i for n in lens for i in range(n)], dtype=torch.int32, device="cuda")
+    seq = torch.tensor([s for s, n in enumerate(lens) for _ in range(n)], dtype=torch.int32, device="cuda")
+    cache = ku.Cache(gen, lens, Hkv, d, page, fp8, fill=False)
+    at = cache.pages[seq.long(), pos.long() // page].long(), pos.long() % page
+
+    def run(x):
+        q = torch.empty((T, Hq, d), dtype=torch.bfloat16, device="cuda")
+        A.kv_append(x.reshape(T, -1), H * d, None, None, 0.0, tab, 64, rot, inter, pos, seq, cache.pages, q, cache.k, cache.v, T, len(lens), Hq, Hkv, d,
+                    cache.width, page, cache.num, A.ATTN_FP8_E4M3 if fp8 else A.ATTN_BF16, 0.25, 0.25)
+        torch.cuda.synchronize()
+        return q, cache.k[at[0], :, at[1]].clone(), cache.v[at[0], :, at[1]].clone()
+
+    got, base = run(x), run(clean)
+    assert _same(got[0][..., rot:], x[:, :Hq, rot:]) and _same(got[0][..., :rot], base[0][..., :rot])
+    k, v = x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    if not fp8:
+        assert _same(got[1][..., rot:], k[..., rot:]) and _same(got[1][..., :rot], base[1][..., :rot]) and _same(got[2], v)
+        return
+    assert torch.equal(got[1][..., :rot], base[1][..., :rot])
+    for codes, want in ((got[1][..., rot:], k[..., rot:]), (got[2], v)):
+        # (a quarter: quotients are exact, so that the code is torch's rounding of the clamped quotient)
+        ref = (want.float() / 0.25).clamp(-448.0, 448.0).to(torch.float8_e4m3fn)
+        nan = want.isnan()
+        assert bool(codes.view(torch.float8_e4m3fn).float()[nan].isnan().all()) and torch.equal(codes[~nan], ref.view(torch.uint8)[~nan])
