@@ -121,7 +121,7 @@ int kv_append(const void* qkv, long long ld, const void* q_weight, const void* k
  * What lies in the cache behind a sequence's last key, or in pages that no visible key names, is never read into a result.
  * Two kernels are enqueued.  The split of the keys over workgroups is computed on the device from `lens`: the call can be captured once and replayed while
  * the sequences grow.  Deterministic.  Products are taken on bf16 with 32-bit sums (e4m3 values are exact in bf16); softmax
- * statistics and sums are 32 bits; the probabilities are rounded to bf16 for the second product.
+ * statistics and sums are 32 bits; a probability enters the second product as the sum of two bf16, 2^-15 of it off.
  */
 int kv_decode(const void* q, const void* k_cache, const void* v_cache, const int* pages, const int* lens,
               void* o, float* lse, void* workspace, int B, int Hq, int Hkv, int d,

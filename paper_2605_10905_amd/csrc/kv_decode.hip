@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
     }
 
     // streaming softmax; differences are taken before they are scaled, so that scores near the type's lowest value do not overflow
-    bf16x8 pr[NQ][NP];
+    bf16x8 pr[NQ][NP], rest[NQ][NP];
 #pragma unroll
     for (int i2 = 0; i2 < NQ; ++i2) {
       float mx = s[i2][0][0];
@@ -463,8 +463,17 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
           e[y] = __builtin_amdgcn_exp2f((s[i2][2 * x + (y >> 2)][y & 3] - ref) * p.scale_log2);
           sum += e[y];
         }
-        // bf16 for the matrix cores: half a step of each probability, as in attn_fwd
-        pr[i2][x] = __builtin_bit_cast(bf16x8, u32x4{attn_pack_bf16(e[0], e[1]), attn_pack_bf16(e[2], e[3]), attn_pack_bf16(e[4], e[5]), attn_pack_bf16(e[6], e[7])});
+        // bf16 for the matrix cores, in two parts: the first eight bits of a probability, and the rest, itself rounded (at most 2^-7 of it,
+        // so off by 2^-15).  2^-18 of it more, so that both parts are positive and an infinite value stays one.
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float e0 = e[2 * y], e1 = e[2 * y + 1], h0 = __uint_as_float(__float_as_uint(e0) & 0xffff0000u), h1 = __uint_as_float(__float_as_uint(e1) & 0xffff0000u);
+          hi[y] = __builtin_amdgcn_perm(__float_as_uint(e1), __float_as_uint(e0), 0x07060302u);
+          lo[y] = attn_pack_bf16(fmaf(e0, 1.f + 0x1p-18f, -h0), fmaf(e1, 1.f + 0x1p-18f, -h1));
+        }
+        pr[i2][x] = __builtin_bit_cast(bf16x8, u32x4{hi[0], hi[1], hi[2], hi[3]});
+        rest[i2][x] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], lo[2], lo[3]});
       }
       l[i2] += sum;  // (of the unrounded probabilities, this lane's keys)
     }
@@ -493,7 +502,10 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
           v = __builtin_bit_cast(bf16x8, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
         }
 #pragma unroll
-        for (int i2 = 0; i2 < NQ; ++i2) o[i2][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[i2][x], o[i2][db], 0, 0, 0);
+        for (int i2 = 0; i2 < NQ; ++i2) {
+          o[i2][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, rest[i2][x], o[i2][db], 0, 0, 0);
+          o[i2][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pr[i2][x], o[i2][db], 0, 0, 0);
+        }
       }
 
     // the slot is free once its last operand has arrived

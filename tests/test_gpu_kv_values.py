@@ -1,9 +1,11 @@
-"""The operators of include/kv.h on the GPU: what particular values become."""
+"""The operators of include/kv.h on the GPU: what particular values become, and how exact the sums of kv_decode are."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import kv_ref as orc
 from tests import kv_util as ku
-from tests.kv_util import NAN
+from tests.kv_util import NAN, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -117,3 +119,68 @@ def test_features_that_are_not_rotated_enter_the_cache_as_they_are(d, rot, inter
         ref = (want.float() / 0.25).clamp(-448.0, 448.0).to(torch.float8_e4m3fn)
         nan = want.isnan()
         assert bool(codes.view(torch.float8_e4m3fn).float()[nan].isnan().all()) and torch.equal(codes[~nan], ref.view(torch.uint8)[~nan])
+
+
+# ---- the sums of kv_decode -----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,fp8", [(4, 2, 128, False), (4, 2, 64, False), (16, 1, 128, True), (5, 1, 64, True), (20, 1, 128, False), (24, 1, 64, True), (40, 1, 64, False),
+                                          (70, 1, 128, True), (64, 1, 128, False)])
+@pytest.mark.parametrize("copies", [1, 24])
+def test_kv_decode_probabilities_keep_more_than_their_first_eight_bits(Hq, Hkv, d, fp8, copies):
+    """Values of both signs, so that an output is small beside sum p |v| and what a probability loses shows.  The bound is decode_check's but for
+    the probabilities: they are the sum of two bf16, the second of which (at most 2^-7 of the probability) is rounded and 2^-18 of it too large:
+    (2^-15 + 2^-18) sum p |v|."""
+    A = _A()
+    lens = [2, 3, 17, 40, 129, 700] * copies
+    gen = ku.generator(211 + Hq)
+    cache = ku.Cache(gen, lens, Hkv, d, 32, fp8)
+    B, scale = len(lens), d ** -0.5
+    q = (torch.randn((B, Hq, d), generator=gen, device="cuda") * 0.25).bfloat16()
+    o, lse = torch.empty_like(q), torch.empty((B, Hq), device="cuda")
+    ws = torch.empty(A.kv_decode_workspace_bytes(B, Hq, Hkv, d) // 4, device="cuda")
+    A.kv_decode(q, cache.k, cache.v, cache.pages, torch.tensor(lens, dtype=torch.int32, device="cuda"), o, lse, ws, B, Hq, Hkv, d, cache.width, 32, cache.num, scale,
+                A.ATTN_FP8_E4M3 if fp8 else A.ATTN_BF16, *cache.descale)
+    torch.cuda.synchronize()
+    got, qd = f64(o), f64(q)
+    for b in range(B):
+        k, v = cache.visible(b)
+        want, want_lse = orc.decode(qd[b], k, v, scale)
+        kk, vv = np.repeat(k, Hq // Hkv, 0), np.repeat(v, Hq // Hkv, 0)
+        p = np.exp(scale * np.einsum("hd,hnd->hn", qd[b], kk) - want_lse[:, None])
+        a = scale * np.einsum("hd,hnd->hn", np.abs(qd[b]), np.abs(kk)).max(-1)
+        rel = 2.0 ** -24 * (2 * (d + 8) * a + k.shape[1] / 16 + 32) + 2.0 ** -20
+        pv = np.einsum("hn,hnd->hd", p, np.abs(vv))
+        bound = (2.0 ** -15 + 2.0 ** -18 + rel[:, None]) * pv * (1 + 2.0 ** -7) + 2.0 ** -8 * np.abs(want) * (1 + 2.0 ** -8) + 1e-38
+        off = np.abs(got[b] - want)
+        assert (off <= bound).all(), (b, lens[b], float((off / bound).max()))
+
+
+@pytest.mark.parametrize("Hq,d", [(4, 128), (4, 64), (20, 128), (40, 64)])
+@pytest.mark.parametrize("value", [INF, -INF])
+def test_kv_decode_infinite_values(Hq, d, value):
+    """p times an infinite value is infinite for every p above zero, those that are bf16 numbers (equal scores: 1) among them, and reaches no other feature."""
+    A = _A()
+    lens = [1, 2, 33, 64, 300]
+    gen = ku.generator(221 + Hq)
+    cache = ku.Cache(gen, lens, 1, d, 16, False)
+    q = (torch.randn((len(lens), Hq, d), generator=gen, device="cuda") * 0.5).bfloat16()
+    q[:, 0] = 0.0  # equal scores
+    lens_ = torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+    def run():
+        o, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        ws = torch.empty(A.kv_decode_workspace_bytes(len(lens), Hq, 1, d) // 4, device="cuda")
+        A.kv_decode(q, cache.k, cache.v, cache.pages, lens_, o, lse, ws, len(lens), Hq, 1, d, cache.width, 16, cache.num, 0.1, A.ATTN_BF16)
+        torch.cuda.synchronize()
+        return o, lse
+
+    clean, clean_lse = run()
+    for b, n in enumerate(lens):
+        cache.v[cache.pages[b, n // 2 // 16].long(), 0, n // 2 % 16, 5 + b] = value
+    o, lse = run()
+    assert torch.equal(lse, clean_lse)
+    for b in range(len(lens)):
+        assert bool((o[b, :, 5 + b] == value).all())
+        keep = [i for i in range(d) if i != 5 + b]
+        assert torch.equal(o[b][:, keep], clean[b][:, keep])
