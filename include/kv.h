@@ -97,7 +97,7 @@ long long rope_qkv_bwd_workspace_bytes(int B, int Hq, int Hkv, int N, int d);
  * page is outside the table (p >= W * page_size) or whose entry is outside 0 .. num_pages - 1 gets its q and does not enter the cache.
  * Tokens of one call must not name the same place of the cache twice: what it then holds is unspecified, and may be a mix.
  * Nothing else of the cache is touched.  One kernel.  Errors as for rope_qkv, and ATTN_ERR_DTYPE, ATTN_ERR_UNSUPPORTED for a
- * page_size, or for a de-scale that is not positive with ATTN_FP8_E4M3.
+ * page_size, or with ATTN_FP8_E4M3 for a de-scale outside 2^-96 .. the largest float32.
  */
 int kv_append(const void* qkv, long long ld, const void* q_weight, const void* k_weight, float eps,
               const float* table, int npos, int rot, int interleaved, const int* pos, const int* seq, const int* pages,
@@ -116,7 +116,8 @@ int kv_append(const void* qkv, long long ld, const void* q_weight, const void* k
  *              o = 0, lse = -inf
  *   workspace  kv_decode_workspace_bytes(B, Hq, Hkv, d) bytes; contents on entry are irrelevant, on return unspecified;
  *              calls that can overlap on the device must not share it
- *   scale      > 0 (ATTN_ERR_UNSUPPORTED otherwise)
+ *   scale      > 0; scale * log2(e), with ATTN_FP8_E4M3 times k_descale, has to be a normal float32, and de-scales as for kv_append
+ *              (ATTN_ERR_UNSUPPORTED otherwise)
  *   d          64 or 128; B * Hq below 2^24 (ATTN_ERR_UNSUPPORTED otherwise)
  * What lies in the cache behind a sequence's last key, or in pages that no visible key names, is never read into a result.
  * Two kernels are enqueued.  The split of the keys over workgroups is computed on the device from `lens`: the call can be captured once and replayed while

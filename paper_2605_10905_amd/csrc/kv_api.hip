@@ -1,4 +1,5 @@
 // C-ABI entry points of the rotary and paged-cache operators: argument checks, launch.  See include/kv.h.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -10,6 +11,9 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 
 bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
+// A de-scale that 32 bits can work with: 1 / sum of up to 2^30 probabilities times it is still a normal number.
+bool descale_fits(float x) { return x >= 0x1p-96f && x <= FLT_MAX; }
 
 // what rope_qkv, its backward and kv_append have in common
 int check_rows(const void* qkv, bool need_qkv, long long ld, const void* wq, const void* wk, float eps, const float* table, int npos, int rot,
@@ -98,7 +102,7 @@ int kv_append(const void* qkv, long long ld, const void* q_weight, const void* k
   if (misaligned(q, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16) || misaligned(pos, 4) || misaligned(seq, 4) || misaligned(pages, 4))
     return ATTN_ERR_SHAPE;
   const bool fp8 = dtype == ATTN_FP8_E4M3;
-  if (fp8 && (!(k_descale > 0.0f) || !(v_descale > 0.0f))) return ATTN_ERR_UNSUPPORTED;
+  if (fp8 && (!descale_fits(k_descale) || !descale_fits(v_descale))) return ATTN_ERR_UNSUPPORTED;
   RopeParams p = row_params(qkv, ld, q_weight, k_weight, eps, table, npos, rot, interleaved, pos, T, 0, Hq, Hkv);
   p.q = q; p.k = k_cache; p.v = v_cache;
   p.seq = seq; p.pages = pages;
@@ -120,12 +124,15 @@ int kv_decode(const void* q, const void* k_cache, const void* v_cache, const int
     return ATTN_ERR_SHAPE;
   if (d != 64 && d != 128) return ATTN_ERR_UNSUPPORTED;
   const bool fp8 = dtype == ATTN_FP8_E4M3;
-  if (!(scale > 0.0f) || (fp8 && (!(k_descale > 0.0f) || !(v_descale > 0.0f)))) return ATTN_ERR_UNSUPPORTED;
+  if (!(scale > 0.0f) || (fp8 && (!descale_fits(k_descale) || !descale_fits(v_descale)))) return ATTN_ERR_UNSUPPORTED;
+  // what the scores are multiplied by: as zero or infinity it would make NaN of a hidden key's -inf, or of the largest score's 0
+  const float scale_log2 = scale * kLog2e * (fp8 ? k_descale : 1.0f);
+  if (!(scale_log2 >= FLT_MIN && scale_log2 <= FLT_MAX)) return ATTN_ERR_UNSUPPORTED;
   if ((long long)B * Hq > 0x00ffffffll) return ATTN_ERR_UNSUPPORTED;  // one workgroup per row has to fit a launch
   DecodeParams p;
   p.q = q; p.k = k_cache; p.v = v_cache; p.pages = pages; p.lens = lens; p.o = o; p.lse = lse; p.ws = workspace;
   p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.W = W; p.page_log2 = __builtin_ctz((unsigned)page_size); p.num_pages = num_pages;
-  p.scale_log2 = scale * kLog2e * (fp8 ? k_descale : 1.0f);
+  p.scale_log2 = scale_log2;
   p.out_scale = fp8 ? v_descale : 1.0f;
   return kv_decode_launch(p, d, fp8, (hipStream_t)stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
