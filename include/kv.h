@@ -63,7 +63,7 @@ int rope_qkv(const void* qkv, long long ld, const void* q_weight, const void* k_
  *     dx = r (g weight - x r mean(g weight x r))              (without weights: dx = g)
  *
  *   dq, dk, dv   bfloat16, layouts of q, k, v
- *   qkv, ld      the forward's input (may be NULL without weights); all arguments to pos as for rope_qkv.  A position outside
+ *   qkv, ld      the forward's input (not used without weights); all arguments to pos as for rope_qkv.  A position outside
  *                the table makes the token's gradients of q and k, and the weights' gradients, NaN
  *   dqkv         bfloat16, rows as qkv's, `dld` elements apart, overwritten (elements between the rows are not touched)
  *   dq_weight, dk_weight   float32 [d], overwritten; not used without weights

@@ -139,10 +139,10 @@ struct Rows {
   int npos, rot, interleaved;
   int* pos;
 };
-Rows rows_of(Args& a, int at, double T, double width, double d) {
+Rows rows_of(Args& a, int at, double T, double width, double d, bool read = true) {  // (read: whether the rows are)
   Rows r;
   r.ld = a.whole(at + 1);
-  r.qkv = a.rows(at, "qkv", r.ld, T, width);
+  r.qkv = read ? a.rows(at, "qkv", r.ld, T, width) : nullptr;
   r.wq = a.bf16(at + 2, "q_weight", d);
   r.wk = a.bf16(at + 3, "k_weight", d);
   r.eps = a.real(at + 4);
@@ -189,12 +189,13 @@ PyObject* py_rope_qkv_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return call<23>("rope_qkv_bwd", v, n, [](Args& a, void* stream) {
     const int B = a.size(18), Hq = a.size(19), Hkv = a.size(20), N = a.size(21), d = a.size(22);
     const double T = (double)B * N, nk = T * Hkv * d, width = ((double)Hq + 2.0 * Hkv) * d;
-    const Rows r = rows_of(a, 3, T, width, d);
+    const bool norm = a.v[5] != Py_None || a.v[6] != Py_None;  // (without weights neither the rows nor the sums are looked at)
+    const Rows r = rows_of(a, 3, T, width, d, norm);
     void *const dq = a.bf16(0, "dq", T * Hq * d), *const dk = a.bf16(1, "dk", nk), *const dv = a.bf16(2, "dv", nk);
     const long long dld = a.whole(14);
     void* const dqkv = a.rows(13, "dqkv", dld, T, width);
-    float *const dwq = a.f32(15, "dq_weight", d), *const dwk = a.f32(16, "dk_weight", d);
-    float* const ws = a.f32(17, "workspace", (double)(rope_qkv_bwd_workspace_bytes(B, Hq, Hkv, N, d) / 4));
+    float *const dwq = norm ? a.f32(15, "dq_weight", d) : nullptr, *const dwk = norm ? a.f32(16, "dk_weight", d) : nullptr;
+    float* const ws = norm ? a.f32(17, "workspace", (double)(rope_qkv_bwd_workspace_bytes(B, Hq, Hkv, N, d) / 4)) : nullptr;
     return a.bad ? 0 : rope_qkv_bwd(dq, dk, dv, r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, dqkv, dld, dwq, dwk, ws, B, Hq, Hkv, N, d, stream);
   });
 }
