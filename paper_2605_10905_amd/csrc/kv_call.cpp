@@ -154,6 +154,17 @@ Rows rows_of(Args& a, int at, double T, double width, double d, bool read = true
   return r;
 }
 
+// Makes the call.  The interpreter is free for other threads meanwhile, as it is inside a ctypes call: a launch waits where the device's queue is
+// full, and what it waits for can need the interpreter.  (The caller's frame holds the arguments.)
+template <typename F, typename... T>
+int made(const Args& a, F function, T... arguments) {
+  if (a.bad) return 0;
+  PyThreadState* const state = PyEval_SaveThread();
+  const int status = function(arguments...);
+  PyEval_RestoreThread(state);
+  return status;
+}
+
 // the first two arguments of every call: the current device, the stream
 template <int COUNT, typename F>
 PyObject* call(const char* name, PyObject* const* v, Py_ssize_t n, F f) {
@@ -181,7 +192,7 @@ PyObject* py_rope_qkv(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const double T = (double)B * N, nk = T * Hkv * d;
     const Rows r = rows_of(a, 0, T, ((double)Hq + 2.0 * Hkv) * d, d);
     void *const q = a.bf16(10, "q", T * Hq * d), *const k = a.bf16(11, "k", nk), *const w = a.bf16(12, "v", nk);
-    return a.bad ? 0 : rope_qkv(r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, q, k, w, B, Hq, Hkv, N, d, stream);
+    return made(a, rope_qkv, r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, q, k, w, B, Hq, Hkv, N, d, stream);
   });
 }
 
@@ -196,7 +207,7 @@ PyObject* py_rope_qkv_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
     void* const dqkv = a.rows(13, "dqkv", dld, T, width);
     float *const dwq = norm ? a.f32(15, "dq_weight", d) : nullptr, *const dwk = norm ? a.f32(16, "dk_weight", d) : nullptr;
     float* const ws = norm ? a.f32(17, "workspace", (double)(rope_qkv_bwd_workspace_bytes(B, Hq, Hkv, N, d) / 4)) : nullptr;
-    return a.bad ? 0 : rope_qkv_bwd(dq, dk, dv, r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, dqkv, dld, dwq, dwk, ws, B, Hq, Hkv, N, d, stream);
+    return made(a, rope_qkv_bwd, dq, dk, dv, r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, dqkv, dld, dwq, dwk, ws, B, Hq, Hkv, N, d, stream);
   });
 }
 
@@ -208,7 +219,7 @@ PyObject* py_kv_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const Rows r = rows_of(a, 0, T, ((double)Hq + 2.0 * Hkv) * d, d);
     int *const seq = a.i32(10, "seq", T), *const pages = a.i32(11, "pages", (double)S * W);
     void *const q = a.bf16(12, "q", (double)T * Hq * d), *const k = a.cache(13, "k_cache", dtype, held), *const w = a.cache(14, "v_cache", dtype, held);
-    return a.bad ? 0 : kv_append(r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, seq, pages, q, k, w, T, S, Hq, Hkv, d, W, page, num, dtype, kd, vd, stream);
+    return made(a, kv_append, r.qkv, r.ld, r.wq, r.wk, r.eps, r.table, r.npos, r.rot, r.interleaved, r.pos, seq, pages, q, k, w, T, S, Hq, Hkv, d, W, page, num, dtype, kd, vd, stream);
   });
 }
 
@@ -221,7 +232,7 @@ PyObject* py_kv_decode(PyObject*, PyObject* const* v, Py_ssize_t n) {
     int *const pages = a.i32(3, "pages", (double)B * W), *const lens = a.i32(4, "lens", B);
     void* const o = a.bf16(5, "o", rows * d);
     float *const lse = a.f32(6, "lse", rows), *const ws = a.f32(7, "workspace", (double)(kv_decode_workspace_bytes(B, Hq, Hkv, d) / 4));
-    return a.bad ? 0 : kv_decode(q, k, w, pages, lens, o, lse, ws, B, Hq, Hkv, d, W, page, num, scale, dtype, kd, vd, stream);
+    return made(a, kv_decode, q, k, w, pages, lens, o, lse, ws, B, Hq, Hkv, d, W, page, num, scale, dtype, kd, vd, stream);
   });
 }
 
