@@ -2,8 +2,10 @@
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -26,44 +28,57 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 SOURCE_FLAGS = {"attn_bwd_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "kv_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
+def _start(cmd, verbose):
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    return cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(cmd, pr, verbose):
+    out, _ = pr.communicate()
+    out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
+    if pr.returncode != 0:
+        raise RuntimeError("the compiler failed:\n" + " ".join(cmd) + "\n" + out)
+    if verbose and out.strip():
+        print(out)
+
+
+def _call_commands():
+    """Compiling and linking the Python side of include/kv.h, or what is missing for it: the libraries are built without it."""
+    try:
+        import torch
+    except ImportError:
+        return None, "torch"
+    where = os.path.dirname(torch.__file__)
+    inc, python = os.path.join(where, "include"), sysconfig.get_path("include")
+    if shutil.which("g++") is None:
+        return None, "g++"
+    for header in (os.path.join(python, "Python.h"), os.path.join(inc, "torch", "csrc", "autograd", "python_variable.h")):
+        if not os.path.exists(header):
+            return None, header
+    obj = os.path.join(CSRC, "kv_call.o")
+    compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-w",
+                "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"), "-I", python, "-c", os.path.join(CSRC, "kv_call.cpp"), "-o", obj]
+    link = ["g++", "-shared", obj, "-o", CALL_KV, f"-L{HERE}", "-lkv_mi355x", f"-L{os.path.join(where, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    return (compile_, link), ""
+
+
 def build(verbose: bool = True, extra_flags=()) -> str:
-    objs = {}
-    procs = []
-    for src in SOURCES + SOURCES_KV:
-        obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-        cmd = [HIPCC, *FLAGS, *SOURCE_FLAGS.get(src, []), *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-        objs[src] = obj
-    import sysconfig
-
-    import torch
-
-    inc = os.path.join(os.path.dirname(torch.__file__), "include")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-w",
-           "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_path("include"),
-           "-c", os.path.join(CSRC, "kv_call.cpp"), "-o", os.path.join(CSRC, "kv_call.o")]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    objs = {src: os.path.join(CSRC, src.replace(".hip", ".o")) for src in SOURCES + SOURCES_KV}
+    procs = [_start([HIPCC, *FLAGS, *SOURCE_FLAGS.get(src, []), *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj], verbose) for src, obj in objs.items()]
+    call, missing = _call_commands()
+    host = _start(call[0], verbose) if call else None
+    if os.path.exists(CALL_KV):
+        os.remove(CALL_KV)  # (never beside a library of another build)
     for cmd, pr in procs:
-        out, _ = pr.communicate()
-        out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
-        if pr.returncode != 0:
-            raise RuntimeError("the compiler failed:\n" + " ".join(cmd) + "\n" + out)
-        if verbose and out.strip():
-            print(out)
+        _finish(cmd, pr, verbose)
     for lib, sources in ((LIB, SOURCES), (LIB_KV, SOURCES_KV)):
-        cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *[objs[src] for src in sources], "-o", lib]
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        subprocess.run(cmd, check=True)
-    tlib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = ["g++", "-shared", os.path.join(CSRC, "kv_call.o"), "-o", CALL_KV, f"-L{HERE}", "-lkv_mi355x", f"-L{tlib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+        _finish(*_start([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *[objs[src] for src in sources], "-o", lib], verbose), verbose)
+    if host is None:
+        print(f"the Python side of include/kv.h is not built: {missing} is missing", file=sys.stderr)
+        return LIB
+    _finish(*host, verbose)
+    _finish(*_start(call[1], verbose), verbose)
     return LIB
 
 
