@@ -14,7 +14,7 @@ SOURCES = ["attn_api.hip", "attn_fwd_sp.hip", "attn_fwd_fp8.hip", "attn_bwd_bf16
 # what stands around attention in a layer (include/kv.h) is a library of its own: who only attends does not load it
 LIB_KV = os.path.join(HERE, "libkv_mi355x.so")
 SOURCES_KV = ["kv_api.hip", "rope.hip", "kv_decode.hip"]
-CALL_KV = os.path.join(HERE, "_kv_call.so")  # its Python side: host code, by the host compiler
+CALL_KV = os.path.join(HERE, "_kv_call" + sysconfig.get_config_var("EXT_SUFFIX"))  # its Python side: host code, by the host compiler, for this Python
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 VALU forms are switched off on purpose (they have misbehaved on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -57,7 +57,7 @@ def _call_commands():
         if not os.path.exists(header):
             return None, header
     obj = os.path.join(CSRC, "kv_call.o")
-    compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-w",
+    compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBUILT_FOR_TORCH="{torch.__version__}"', "-w",
                 "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"), "-I", python, "-c", os.path.join(CSRC, "kv_call.cpp"), "-o", obj]
     link = ["g++", "-shared", obj, "-o", CALL_KV, f"-L{HERE}", "-lkv_mi355x", f"-L{os.path.join(where, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
     return (compile_, link), ""

@@ -247,4 +247,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_call", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__kv_call() { return PyModule_Create(&module); }
+// (tensors are read by their layout in memory: built_for_torch, the version that this was built for, is compared by kv.py)
+PyMODINIT_FUNC PyInit__kv_call() {
+  PyObject* const m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for_torch", BUILT_FOR_TORCH) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

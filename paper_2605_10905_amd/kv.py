@@ -11,19 +11,24 @@ import torch
 
 from .binding import HERE, AttnError
 from .binding import _stream as _stream_of
+from .build import CALL_KV
 
 lib_path = os.path.join(HERE, "libkv_mi355x.so")
+_BUILD = "build it first with `python -m paper_2605_10905_amd.build` (there is no fallback path)"
 
 
 def _load():
-    for path in (lib_path, os.path.join(HERE, "_kv_call.so")):
+    for path in (lib_path, CALL_KV):
         if not os.path.exists(path):
-            raise ImportError(f"{path} is missing: build it first with `python -m paper_2605_10905_amd.build` (there is no fallback path)")
+            raise ImportError(f"{path} is missing: {_BUILD}")
     return C.CDLL(lib_path)
 
 
 lib = _load()
 from . import _kv_call as _call  # noqa: E402  (after the library that it calls)
+
+if _call.built_for_torch != torch.__version__:  # (it reads tensors by their layout in memory)
+    raise ImportError(f"{CALL_KV} was built for torch {_call.built_for_torch}, this is {torch.__version__}: {_BUILD}")
 
 _i, _ll = C.c_int, C.c_longlong
 lib.rope_qkv_bwd_workspace_bytes.argtypes = [_i] * 5

@@ -1,11 +1,15 @@
-"""The libraries need hipcc alone; the Python side of include/kv.h, which needs more, does not stand in their way."""
+"""The libraries need hipcc alone; the Python side of include/kv.h, which needs more, does not stand in their way, and is only loaded by
+the Python and torch that it was built for."""
 import importlib
 import os
 import stat
+import subprocess
 import sys
 import sysconfig
 
 import pytest
+
+from tests.test_kv_abi import ROOT, A  # noqa: F401  (A: the fixture)
 
 _TOOL = """#!/bin/sh
 # writes the name of its output into it
@@ -77,3 +81,15 @@ def test_a_kernel_that_does_not_compile_is_an_error(build, tmp_path):
     _tool(tmp_path / "hipcc", "#!/bin/sh\necho wrong; exit 1\n")
     with pytest.raises(RuntimeError, match="wrong"):
         build.build(verbose=False)
+
+
+def test_the_python_side_names_its_python(A):  # noqa: F811
+    call = importlib.import_module("paper_2605_10905_amd.kv")._call
+    assert call.__file__.endswith(sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def test_the_python_side_of_another_torch_is_refused(A):  # noqa: F811
+    """Tensors are read by their layout in memory, which another torch may have changed."""
+    code = "import torch; torch.__version__ = '0.0.1'; import paper_2605_10905_amd as A; A.attn_version(); A.kv_decode"
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=120)
+    assert r.returncode != 0 and "ImportError" in r.stderr and "0.0.1" in r.stderr, r.stderr[-500:]
