@@ -155,7 +155,10 @@ __device__ __forceinline__ bf16x8 e4m3_to_bf16(uint32_t lo, uint32_t hi) {  // (
 __host__ __device__ constexpr int blocks_for(int G) { return G <= 16 ? 1 : G <= 32 ? 2 : 4; }
 __host__ __device__ __forceinline__ int rows_kept(int G) { return G < 16 * blocks_for(G) ? G : 16 * blocks_for(G); }
 // floats of one wave's sums: rows of O, then (reference maximum, sum) of each row
-__host__ __device__ __forceinline__ int partial_floats(int rows, int d) { return rows * d + (2 * rows + 3) / 4 * 4; }
+template <typename I>
+__host__ __device__ __forceinline__ I partial_floats(int rows, I d) {
+  return rows * d + (2 * rows + 3) / 4 * 4;
+}
 // What the second kernel has to know of each (sequence, unit), behind the sums: written by the wave that takes its first tile (first)
 // and, where that is another one, by the wave that takes its last (last).
 struct Split {
@@ -164,7 +167,10 @@ struct Split {
   int ends;   // (with last) whether that wave's piece ends with this (sequence, unit)
   int step;   // (with first) waves from one with a part to the next
 };
-__host__ __device__ __forceinline__ size_t split_offset(int rows, int d) { return (size_t)2 * kWorkers * partial_floats(rows, d) * sizeof(float); }
+template <typename I>
+__host__ __device__ __forceinline__ size_t split_offset(int rows, I d) {
+  return (size_t)2 * kWorkers * partial_floats(rows, d) * sizeof(float);
+}
 
 // JOINT: whether a workgroup's waves add their sums where they can (see the end).
 template <int D, bool FP8, int NQ, bool JOINT>
@@ -746,7 +752,8 @@ int kv_decode_launch(const DecodeParams& p, int d, bool fp8, hipStream_t stream)
   return sums_are_added(segments) ? launch<true>(p, d, fp8, nq, segments, stream) : launch<false>(p, d, fp8, nq, segments, stream);
 }
 
-long long kv_decode_bytes(int B, int Hq, int Hkv, int d) {
+long long kv_decode_bytes(int B, int Hq, int Hkv, int d) {  // (of any sizes, those that no call takes among them)
   const int G = Hq / Hkv, nq = blocks_for(G);
-  return (long long)split_offset(rows_kept(G), d) + (long long)B * Hkv * ((G + 16 * nq - 1) / (16 * nq)) * (long long)sizeof(Split);
+  const long long segments = (long long)B * (Hkv * ((G - 1) / (16 * nq) + 1ll)), most = 1 << 24;  // (no call has more)
+  return (long long)split_offset(rows_kept(G), (long long)d) + (segments < most ? segments : most) * (long long)sizeof(Split);
 }

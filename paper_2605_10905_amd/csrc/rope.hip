@@ -459,7 +459,9 @@ int kv_append_launch(const RopeParams& p, int d, bool fp8, hipStream_t stream) {
 }
 
 int rope_qkv_bwd_workgroups(long long T, long long heads, int d) {
-  const long long per = d >= 1024 ? 1 : 1024 / d, tasks = (T * heads + per - 1) / per, wgs = (tasks + kWaves - 1) / kWaves;
+  constexpr long long kEnough = kMostPartials * kWaves * (1024 / 64);  // tokens or heads that take every workgroup (so that any product fits)
+  const long long rows = (T < kEnough ? T : kEnough) * (heads < kEnough ? heads : kEnough);
+  const long long per = d >= 1024 ? 1 : 1024 / d, tasks = (rows + per - 1) / per, wgs = (tasks + kWaves - 1) / kWaves;
   return (int)(wgs < kMostPartials ? wgs : kMostPartials);
 }
 

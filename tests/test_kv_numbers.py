@@ -42,3 +42,13 @@ def test_what_can_be_computed_is_taken(tmp_path):
     got, _ = _routes(tmp_path, calls)
     for (name, kw), (st, launches) in zip(calls, got):
         assert st == 0 and len(launches) == (2 if name == "kv_decode" else 1), (name, kw, st)
+
+
+def test_workspace_sizes_of_sizes_that_no_call_takes(A):  # noqa: F811
+    """They do not wrap around: enough, or as much as the largest call needs."""
+    big = 2 ** 31 - 1
+    assert A.rope_qkv_bwd_workspace_bytes(big, big, big, big, 128) == A.rope_qkv_bwd_workspace_bytes(64, 64, 64, 1 << 20, 128)
+    assert A.rope_qkv_bwd_workspace_bytes(1, 1, 1, 1, big) == 2 * 4 * big
+    for shape in ((1, 1, 1, 2 ** 27), (1, 64, 1, 2 ** 26), (big, 64, 1, 128), (big, big, 1, 64), (big, big, big, 64)):
+        B, Hq, Hkv, d = shape
+        assert A.kv_decode_workspace_bytes(*shape) >= 2 * 1024 * min(Hq // Hkv, 16) * d * 4, shape
