@@ -53,6 +53,8 @@ def _stream(stream, device):
             return torch._C._cuda_getCurrentRawStream(device)  # (the handle alone, as the other calls take it)
         except (AttributeError, RuntimeError):
             pass
+    elif getattr(stream, "device_index", device) != device:
+        raise ValueError(f"the stream is on device {stream.device_index}, the current one is {device}")
     return _stream_of(stream) or 0
 
 
