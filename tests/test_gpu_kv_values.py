@@ -184,3 +184,51 @@ def test_kv_decode_infinite_values(Hq, d, value):
         assert bool((o[b, :, 5 + b] == value).all())
         keep = [i for i in range(d) if i != 5 + b]
         assert torch.equal(o[b][:, keep], clean[b][:, keep])
+
+
+# ---- captured calls ------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_captured_rope_and_its_backward_follow_their_inputs(norm):
+    """rope_qkv and rope_qkv_bwd in one graph, replayed over other rows, positions, gradients and weights, with eager calls between."""
+    A = _A()
+    B, N, Hq, Hkv, d, npos = 2, 301, 6, 2, 128, 400
+    gen = ku.generator(231)
+    T, width, tab = B * N, (Hq + 2 * Hkv) * d, ku.table(npos, d)
+    heads = (Hq, Hkv, Hkv)
+
+    def buffers():
+        dws = [torch.empty(d, device="cuda") if norm else None for _ in range(2)]
+        ws = torch.full((A.rope_qkv_bwd_workspace_bytes(B, Hq, Hkv, N, d) // 4,), NAN, device="cuda") if norm else None
+        return [torch.empty((B, h, N, d), dtype=torch.bfloat16, device="cuda") for h in heads], torch.empty((T, width), dtype=torch.bfloat16, device="cuda"), dws, ws
+
+    def inputs():
+        return (ku.rows(gen, T, width, width), ku.weights(gen, d, norm), torch.randint(0, npos, (T,), generator=gen, device="cuda", dtype=torch.int32),
+                [torch.randn((B, h, N, d), generator=gen, device="cuda").bfloat16() for h in heads])
+
+    def call(inp, buf):
+        (qkv, w, pos, grads), (outs, dqkv, dws, ws) = inp, buf
+        A.rope_qkv(qkv, width, *w, 1e-5, tab, npos, d, False, pos, *outs, B, Hq, Hkv, N, d)
+        A.rope_qkv_bwd(*grads, qkv, width, *w, 1e-5, tab, npos, d, False, pos, dqkv, width, *dws, ws, B, Hq, Hkv, N, d)
+
+    flat = lambda x: [t for y in x for t in (y if isinstance(y, list) else [y]) if t is not None]
+    held, got, eager = inputs(), buffers(), buffers()
+    call(held, got)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(held, got)
+    for _ in range(4):
+        new = inputs()
+        for dst, src in zip(flat(held), flat(new)):
+            dst.copy_(src)
+        for t in flat(got):
+            t.fill_(7.0)
+        graph.replay()
+        call(new, eager)
+        torch.cuda.synchronize()
+        for x, y in zip(flat(got[:3]), flat(eager[:3])):
+            assert torch.equal(x, y)
