@@ -23,8 +23,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # the one-wave-per-SIMD backward kernel keeps its score accumulators in ordinary registers, where the vector work reads them.
 # (An internal switch of the compiler: known to the clang 22 of ROCm 7.2.0, with which all figures were taken.  A compiler that does not know
 # it refuses the build; without it the kernels' register plan does not hold, and the listing has to be read anew for the wait states.)
-# kv_decode.hip, one wave per SIMD too: its products in ordinary registers save 90 register moves a tile (16 x 2000 keys 25.7 -> 25.3 us,
-# 1 x 500 4.8 -> 4.4); nothing there depends on it.
+# kv_decode.hip, one wave per SIMD too: its products in ordinary registers save 90 register moves a tile.  Calls without / with it, us: 1 x 500 keys
+# 8.4 / 8.2, 24 ragged up to 1500, d = 64 21.6 / 21.0, 32 up to 9000, e4m3 67.7 / 66.3; groups of 64 queries, 64 x 4000 46.3 / 44.7, e4m3 35.3 / 31.6.
+# Nothing there depends on it.
 SOURCE_FLAGS = {"attn_bwd_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "kv_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

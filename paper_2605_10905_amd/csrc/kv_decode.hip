@@ -1,11 +1,17 @@
 // Attention of one new token per sequence over the paged cache (kv_decode).
 //
-// The call reads every visible key and value once and does 4 G operations on each of their features (G query heads share a
-// key head), so it is bound by memory as long as the products run on the matrix cores and enough bytes are in flight.
+// The call reads every visible key and value once and does 2 G operations on each feature of a key and 4 G on each of a value (G query heads
+// share a key head), so it is bound by memory as long as the products run on the matrix cores and enough bytes are in flight.  A wave holds
+// 64 queries at most: keys and values are read ceil(G / 64) times.
 //
 // Measured, where a 1 GiB device copy runs at 5.16 TB/s (keys and values read a second, both kernels): 2 x 131072 keys, 64/8 heads, d = 128
-// 188 us (5.7 TB/s); 64 ragged sequences up to 6000 151 (5.4); 32 up to 9000, e4m3 65 (4.7); 24 up to 1500, 16/16 heads, d = 64 20.7 (3.7);
-// 1 x 500, 32/8 heads 7.8, which is two launches.
+// 188 - 190 us (5.7 TB/s); 64 ragged sequences up to 6000 151 - 152 (5.4); 32 up to 9000, e4m3 65.5 - 66.3 (4.6); 24 up to 1500, 16/16 heads, d = 64
+// 20.5 - 21 (3.7); 1 x 500, 32/8 heads 8.2, which is two launches.  Groups of 64 queries, 64 x 4000 keys, 64/1 heads: d = 128 44.7 (2.9), e4m3 31.6
+// (2.1); d = 64 24.5 (2.7), e4m3 22.0 (1.5): bound by the vector work of 64 rows, not by memory.
+//
+// Probabilities enter the second product as two bf16 (see there).  Rounded to one, which put o 19 - 35 % further off the definition, the same calls
+// took 187 - 190, 150 - 152, 65.1 - 65.6, 20.2 - 20.6, 8.1; 42.6, 29.0; 22.9, 20.0.  The figures beside the choices below were taken with one: they
+// compare the two sides.
 //
 // Split: the work is the list of all tiles (8 KB of keys: 32, 64 or 128 of them, and their values), sequence by sequence, key head by
 // key head; each of kWorkers waves takes an equal, consecutive piece of it, whatever the lengths are.  What the pieces are follows from
