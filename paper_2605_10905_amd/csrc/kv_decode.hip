@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(kWaves * 64, 1) kv_decode_kernel(const DecodeP
           sum += e[y];
         }
         // bf16 for the matrix cores, in two parts: the first eight bits of a probability, and the rest, itself rounded (at most 2^-7 of it,
-        // so off by 2^-15).  2^-18 of it more, so that both parts are positive and an infinite value stays one.
+        // so off by 2^-15).  2^-18 of it more, so that both parts are positive, as numbers of bf16 above 2^-108, and an infinite value stays one.
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
